@@ -355,6 +355,121 @@ enum { SSMV_PROBE_READ = 0, SSMV_PROBE_WRITE = 1, SSMV_PROBE_R1W1 = 2, SSMV_PROB
 int ssmv_stream_probe(int32_t mode, const void *src, void *dst0, void *dst1, size_t n_bytes, int32_t piece_kib, int32_t grid,
                       void *hip_stream);
 
+/* ---- plain and beam decoding -----------------------------------------------------------------------------------------
+ * The calls below move a sequence from state to state without a cache: no window, no snapshots, no commit.  The state of
+ * a sequence is the pair that ssmv_cache_reset takes: h [H][P][N] fp32 row-major, and conv [3][channels] io_dtype, the
+ * newest raw conv inputs, oldest first.  (ssmv_materialize gives h of a cache, ssmv_conv_history its conv.)  States are
+ * arrays of rows; a call reads one array and writes another, or the same one where no src_row is given.
+ *
+ * src_row (device int32 [batch], or NULL): row b continues from row src_row[b] of the state that goes in - several rows may
+ * continue from the same one, as the beams of a search do - and becomes row b of the state that comes out.  An index
+ * outside [0, rows_in) stands for an empty start: zeros.  NULL: row b.
+ *
+ * Strides are in elements, between a sequence's tokens (or the rows of a single-token call); 0 = packed.  Sequences are L
+ * strides apart, so that x and z, or B and C, may be parts of one projection's output.  Tensors of these calls need only the
+ * alignment of their elements, but B and C rows 4 bytes; where all are 16-byte aligned, strides and channels too, accesses are
+ * 16 bytes wide.  States (h_in, h_out), A and the workspaces: 16 bytes.  No output may overlap an input, but where it is said. */
+
+/* The causal depthwise convolution of conv1d_state_update over L tokens (L = 1: one new token of every row):
+ *   out[b][t][c] = act(bias[c] + sum_{w<4} wgt[c][w] * raw_b[t-3+w][c]),  raw_b = the history of row src_row[b], then x[b],
+ * accumulated in fp32 and rounded to io_dtype.  conv_out receives the newest three raw inputs; it may be conv_in where
+ * src_row is NULL.  seq_len (device int32 [batch] or NULL = L): sequence b has clamp(seq_len[b], 0, L) tokens; what lies behind
+ * them is neither read nor written. */
+typedef struct ssmv_conv_args {
+    const void *x;           /* [batch][L][channels] io_dtype                                     */
+    const void *wgt;         /* [channels][4] io_dtype                                            */
+    const void *bias;        /* [channels] io_dtype or NULL                                       */
+    const void *conv_in;     /* [rows_in][3][channels] io_dtype, or NULL: an empty history        */
+    const int32_t *src_row;  /* [batch] or NULL                                                   */
+    const int32_t *seq_len;  /* [batch] or NULL                                                   */
+    void *out;               /* [batch][L][channels] io_dtype                                     */
+    void *conv_out;          /* [batch][3][channels] io_dtype, or NULL: not wanted                */
+    int64_t x_stride, out_stride;
+    int32_t batch, rows_in, channels, L, io_dtype, act;   /* rows_in 0: batch                     */
+} ssmv_conv_args;
+int ssm_causal_conv(const ssmv_conv_args *args, void *hip_stream);
+
+/* A prompt through the recurrence with a decay per channel and state index (a_mode DIAG), from state to state:
+ *   dt' = softplus(dt + dt_bias) (dt_softplus = 1; else dt' = dt);  h <- exp(dt' * A) * h + (dt' * x) * B_t;
+ *   y = C_t . h + D * x,  y <- y * z * sigmoid(z) where z is given
+ * in fp32, y rounded once to io_dtype.  x is the conv's output.  dstate in {16, 32, 64}.  seq_len as above: h_out is
+ * the state after a sequence's own tokens.
+ * Few sequences and channels and a long prompt: the prompt is cut into segments that run side by side; their end states need
+ * `workspace` (ssm_selective_scan_workspace bytes, 0 where nothing is cut; SSMV_EINVAL where it is needed and NULL).  The cut depends on
+ * batch, channels, dstate and L only; the same call gives the same bits. */
+typedef struct ssmv_scan_args {
+    const void *x;           /* [batch][L][channels] io_dtype                                     */
+    const void *dt;          /* [batch][L][channels] io_dtype                                     */
+    const float *dt_bias;    /* [channels] fp32 or NULL                                           */
+    const float *A;          /* [channels][dstate] fp32, negative                                 */
+    const void *Bm;          /* [batch][L][dstate] io_dtype                                       */
+    const void *Cm;          /* [batch][L][dstate] io_dtype                                       */
+    const float *D;          /* [channels] fp32                                                   */
+    const void *z;           /* [batch][L][channels] io_dtype or NULL                             */
+    const float *h_in;       /* [rows_in][channels][dstate] fp32, or NULL: zeros                  */
+    const int32_t *src_row;  /* [batch] or NULL                                                   */
+    const int32_t *seq_len;  /* [batch] or NULL                                                   */
+    void *y_out;             /* [batch][L][channels] io_dtype                                     */
+    float *h_out;            /* [batch][channels][dstate] fp32, or NULL: not wanted; may be h_in where src_row is NULL */
+    void *workspace;
+    int64_t x_stride, dt_stride, b_stride, c_stride, z_stride, y_stride;
+    int32_t batch, rows_in, channels, dstate, L, io_dtype, dt_softplus;
+} ssmv_scan_args;
+int ssm_selective_scan(const ssmv_scan_args *args, void *hip_stream);
+int ssm_selective_scan_workspace(int32_t batch, int32_t channels, int32_t dstate, int32_t L, size_t *out_bytes);
+
+/* One token of every row through the recurrence, from state to state: a_mode DIAG as above (headdim 1, ngroups 1, dstate <= 64), or
+ * SCALAR with one step and one decay per head and grouped B and C as in ssm_verify_multistep (dstate up to 256).  h_out may be h_in
+ * where src_row is NULL. */
+typedef struct ssmv_token_args {
+    const void *x;           /* [rows][H*P] io_dtype: the conv's output                           */
+    const void *dt;          /* [rows][H] io_dtype                                                */
+    const float *dt_bias;    /* [H] fp32 or NULL                                                  */
+    const float *A;          /* [H] or [H][N] fp32, negative                                      */
+    const void *Bm;          /* [rows][G][N] io_dtype                                             */
+    const void *Cm;          /* [rows][G][N] io_dtype                                             */
+    const float *D;          /* [H] fp32                                                          */
+    const void *z;           /* [rows][H*P] io_dtype or NULL                                      */
+    const float *h_in;       /* [rows_in][H][P][N] fp32, or NULL: zeros                           */
+    const int32_t *src_row;  /* [rows] or NULL                                                    */
+    void *y_out;             /* [rows][H*P] io_dtype                                              */
+    float *h_out;            /* [rows][H][P][N] fp32                                              */
+    int64_t x_stride, dt_stride, b_stride, c_stride, z_stride, y_stride;
+    int32_t rows, rows_in, nheads, headdim, dstate, ngroups, io_dtype, a_mode, dt_softplus;
+} ssmv_token_args;
+int ssm_selective_step(const ssmv_token_args *args, void *hip_stream);
+
+/* Beam search's choice: of the candidates (row r, token v) of every sequence's beams_in rows, with the score
+ *   scores[r] + logits[r][v] - logsumexp(logits[r])     (differences and sums of candidates in 64 bits),
+ * the beams_out best, best first; equal scores by the lower row, inside a row by the higher logit, then the lower token.
+ * parent holds rows of the whole batch (sequence * beams_in + beam), ready to be the src_row of the next step's calls.
+ *   - done (device int32 [batch*beams_in], or NULL): a row with done != 0 is a finished hypothesis: its logits are not read, its
+ *     one candidate is itself, token `eos` with its score unchanged (further places of it: eos with score -inf).  done_out
+ *     (or NULL): 1 where the parent was finished or the token is eos.
+ *   - a logit of -inf (or NaN) is a token that is not allowed: score -inf, chosen only where nothing else is left, also where
+ *     a row allows nothing at all.  +inf counts as the largest finite fp32.  A NaN in scores counts as -inf.
+ * logits io_dtype, rows row_stride apart (0 = vocab).  beams_in, beams_out in [1, SSMV_BEAMS_MAX], beams_out <=
+ * beams_in * vocab; eos in [0, vocab), or -1 = none (not with done).  workspace: ssmv_beam_workspace bytes. */
+#define SSMV_BEAMS_MAX 64
+typedef struct ssmv_beam_args {
+    const void *logits;      /* [batch*beams_in][vocab] io_dtype                                  */
+    const float *scores;     /* [batch*beams_in] fp32                                             */
+    const int32_t *done;     /* [batch*beams_in] or NULL                                          */
+    int32_t *parent;         /* [batch*beams_out]                                                 */
+    int32_t *token;          /* [batch*beams_out]                                                 */
+    float *scores_out;       /* [batch*beams_out]                                                 */
+    int32_t *done_out;       /* [batch*beams_out] or NULL                                         */
+    void *workspace;
+    int64_t row_stride;
+    int32_t batch, beams_in, beams_out, vocab, io_dtype, eos;
+} ssmv_beam_args;
+int ssmv_beam_select(const ssmv_beam_args *args, void *hip_stream);
+int ssmv_beam_workspace(int32_t batch, int32_t beams_in, int32_t beams_out, int32_t vocab, size_t *out_bytes);
+
+/* The conv part of a cache's state: the newest three raw inputs at pos+pend, oldest first, to conv_out [batch][3][Cx]
+ * io_dtype device (the counterpart of ssmv_materialize; the cache is not changed). */
+int ssmv_conv_history(const ssmv_dims *dims, const ssmv_cache *cache, void *conv_out, void *hip_stream);
+
 const char *ssmv_last_error(void);
 const char *ssmv_version(void);
 

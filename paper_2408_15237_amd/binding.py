@@ -24,6 +24,7 @@ SSMV_WINDOW = 16
 SSMV_KMAX_LIMIT = 16
 SSMV_CONV_WIDTH = 4
 SSMV_CACHE_NPTR = 15
+SSMV_BEAMS_MAX = 64
 
 IO_CODES = {"f32": SSMV_F32, "bf16": SSMV_BF16}
 MODE_CODES = {"scalar": SSMV_A_SCALAR, "diag": SSMV_A_DIAG}
@@ -35,7 +36,8 @@ ENGINE_CODES = {"auto": SSMV_ENGINE_AUTO, "vector": SSMV_ENGINE_VECTOR}
 EXPORTS = [
     "ssmv_cache_sizes", "ssmv_cache_reset", "conv1d_state_update", "ssm_verify_multistep",
     "ssm_conv_verify_multistep", "ssm_block_multistep", "ssmv_materialize_block", "ssm_prefill_chunked", "ssm_prefill_block", "ssm_commit_rollback", "ssm_commit_rollback_multi", "ssmv_materialize", "ssmv_first_conflict", "ssmv_gated_rmsnorm", "ssmv_check",
-    "ssmv_set_tuning", "ssmv_copy_probe", "ssmv_stream_probe", "ssmv_engine_of", "ssmv_last_error", "ssmv_version",
+    "ssm_causal_conv", "ssm_selective_scan", "ssm_selective_scan_workspace", "ssm_selective_step", "ssmv_beam_select", "ssmv_beam_workspace",
+    "ssmv_conv_history", "ssmv_set_tuning", "ssmv_copy_probe", "ssmv_stream_probe", "ssmv_engine_of", "ssmv_last_error", "ssmv_version",
 ]
 
 
@@ -49,6 +51,23 @@ class ssmv_prefill_args(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in (
         "x_raw", "conv_wgt", "conv_bias", "dt", "dt_bias", "Bm", "Cm", "z", "A", "D", "seq_len", "y_out")] + [
         (n, ctypes.c_int32) for n in ("L", "dt_softplus")]
+
+
+def _args_struct(name, pointers, longs, ints):
+    return type(name, (ctypes.Structure,), {"_fields_": [(n, ctypes.c_void_p) for n in pointers] + [(n, ctypes.c_int64) for n in longs] +
+                                            [(n, ctypes.c_int32) for n in ints]})
+
+
+ssmv_conv_args = _args_struct("ssmv_conv_args", ("x", "wgt", "bias", "conv_in", "src_row", "seq_len", "out", "conv_out"), ("x_stride", "out_stride"),
+                              ("batch", "rows_in", "channels", "L", "io_dtype", "act"))
+ssmv_scan_args = _args_struct("ssmv_scan_args", ("x", "dt", "dt_bias", "A", "Bm", "Cm", "D", "z", "h_in", "src_row", "seq_len", "y_out", "h_out", "workspace"),
+                              ("x_stride", "dt_stride", "b_stride", "c_stride", "z_stride", "y_stride"),
+                              ("batch", "rows_in", "channels", "dstate", "L", "io_dtype", "dt_softplus"))
+ssmv_token_args = _args_struct("ssmv_token_args", ("x", "dt", "dt_bias", "A", "Bm", "Cm", "D", "z", "h_in", "src_row", "y_out", "h_out"),
+                               ("x_stride", "dt_stride", "b_stride", "c_stride", "z_stride", "y_stride"),
+                               ("rows", "rows_in", "nheads", "headdim", "dstate", "ngroups", "io_dtype", "a_mode", "dt_softplus"))
+ssmv_beam_args = _args_struct("ssmv_beam_args", ("logits", "scores", "done", "parent", "token", "scores_out", "done_out", "workspace"), ("row_stride",),
+                              ("batch", "beams_in", "beams_out", "vocab", "io_dtype", "eos"))
 
 
 class SsmvError(RuntimeError):
@@ -112,6 +131,12 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.ssmv_materialize_block.argtypes = [dp, cp, vp, vp, i32, vp, vp]
     lib.ssmv_first_conflict.argtypes = [vp, vp, i32, i32, vp, vp]
     lib.ssmv_gated_rmsnorm.argtypes = [vp, vp, vp, i32, i32, i32, ctypes.c_float, i32, vp, vp]
+    for name, args in (("ssm_causal_conv", ssmv_conv_args), ("ssm_selective_scan", ssmv_scan_args), ("ssm_selective_step", ssmv_token_args),
+                       ("ssmv_beam_select", ssmv_beam_args)):
+        getattr(lib, name).argtypes = [ctypes.POINTER(args), vp]
+    lib.ssm_selective_scan_workspace.argtypes = [i32, i32, i32, i32, ctypes.POINTER(sz)]
+    lib.ssmv_beam_workspace.argtypes = [i32, i32, i32, i32, ctypes.POINTER(sz)]
+    lib.ssmv_conv_history.argtypes = [dp, cp, vp, vp]
     lib.ssmv_check.argtypes = [cp, vp]
     lib.ssmv_set_tuning.argtypes = [i32, i32]
     lib.ssmv_copy_probe.argtypes = [vp, vp, vp, sz, vp]
@@ -254,6 +279,61 @@ def ssmv_first_conflict(draft, target, batch: int, k: int, accepted, stream=None
 def ssmv_gated_rmsnorm(y, z, weight, rows: int, channels: int, group_size: int, eps: float, io, out, stream=None) -> None:
     _ck(load_library().ssmv_gated_rmsnorm(_ptr(y), _ptr(z), _ptr(weight), rows, channels, group_size, eps,
                                           IO_CODES[io] if isinstance(io, str) else io, _ptr(out), _stream(stream)))
+
+
+# ---- plain and beam decoding: from state to state -----------------------------------------------------------------------
+
+def _rows(t, rows_in, default: int) -> int:
+    """Rows of the state that goes in: as given, else the tensor's first dimension, else as many as go out."""
+    return rows_in if rows_in else t.shape[0] if hasattr(t, "shape") else default
+
+
+def ssm_causal_conv(*, x, wgt, out, batch: int, channels: int, L: int, io, bias=None, act="none", conv_in=None, conv_out=None, src_row=None,
+                    rows_in: int = 0, seq_len=None, x_stride: int = 0, out_stride: int = 0, stream=None) -> None:
+    a = ssmv_conv_args(_ptr(x), _ptr(wgt), _ptr(bias), _ptr(conv_in), _ptr(src_row), _ptr(seq_len), _ptr(out), _ptr(conv_out), x_stride, out_stride,
+                       batch, _rows(conv_in, rows_in, batch), channels, L, IO_CODES.get(io, io), ACT_CODES.get(act, act))
+    _ck(load_library().ssm_causal_conv(ctypes.byref(a), _stream(stream)))
+
+
+def ssm_selective_scan_workspace(batch: int, channels: int, dstate: int, L: int) -> int:
+    out = ctypes.c_size_t()
+    _ck(load_library().ssm_selective_scan_workspace(batch, channels, dstate, L, ctypes.byref(out)))
+    return out.value
+
+
+def ssm_selective_scan(*, x, dt, A, Bm, Cm, D, y_out, batch: int, channels: int, dstate: int, L: int, io, dt_bias=None, dt_softplus: bool = False,
+                       z=None, h_in=None, h_out=None, src_row=None, rows_in: int = 0, seq_len=None, x_stride: int = 0, dt_stride: int = 0,
+                       b_stride: int = 0, c_stride: int = 0, z_stride: int = 0, y_stride: int = 0, workspace=None, stream=None) -> None:
+    a = ssmv_scan_args(_ptr(x), _ptr(dt), _ptr(dt_bias), _ptr(A), _ptr(Bm), _ptr(Cm), _ptr(D), _ptr(z), _ptr(h_in), _ptr(src_row), _ptr(seq_len),
+                       _ptr(y_out), _ptr(h_out), _ptr(workspace), x_stride, dt_stride, b_stride, c_stride, z_stride, y_stride,
+                       batch, _rows(h_in, rows_in, batch), channels, dstate, L, IO_CODES.get(io, io), dt_softplus)
+    _ck(load_library().ssm_selective_scan(ctypes.byref(a), _stream(stream)))
+
+
+def ssm_selective_step(*, x, dt, A, Bm, Cm, D, y_out, h_in, h_out, rows: int, nheads: int, headdim: int, dstate: int, io, ngroups: int = 1,
+                       a_mode="scalar", dt_bias=None, dt_softplus: bool = False, z=None, src_row=None, rows_in: int = 0, x_stride: int = 0,
+                       dt_stride: int = 0, b_stride: int = 0, c_stride: int = 0, z_stride: int = 0, y_stride: int = 0, stream=None) -> None:
+    a = ssmv_token_args(_ptr(x), _ptr(dt), _ptr(dt_bias), _ptr(A), _ptr(Bm), _ptr(Cm), _ptr(D), _ptr(z), _ptr(h_in), _ptr(src_row), _ptr(y_out),
+                        _ptr(h_out), x_stride, dt_stride, b_stride, c_stride, z_stride, y_stride, rows, _rows(h_in, rows_in, rows),
+                        nheads, headdim, dstate, ngroups, IO_CODES.get(io, io), MODE_CODES.get(a_mode, a_mode), dt_softplus)
+    _ck(load_library().ssm_selective_step(ctypes.byref(a), _stream(stream)))
+
+
+def ssmv_beam_workspace(batch: int, beams_in: int, beams_out: int, vocab: int) -> int:
+    out = ctypes.c_size_t()
+    _ck(load_library().ssmv_beam_workspace(batch, beams_in, beams_out, vocab, ctypes.byref(out)))
+    return out.value
+
+
+def ssmv_beam_select(*, logits, scores, parent, token, scores_out, batch: int, beams_in: int, beams_out: int, vocab: int, io, workspace,
+                     row_stride: int = 0, done=None, done_out=None, eos: int = -1, stream=None) -> None:
+    a = ssmv_beam_args(_ptr(logits), _ptr(scores), _ptr(done), _ptr(parent), _ptr(token), _ptr(scores_out), _ptr(done_out), _ptr(workspace), row_stride,
+                       batch, beams_in, beams_out, vocab, IO_CODES.get(io, io), eos)
+    _ck(load_library().ssmv_beam_select(ctypes.byref(a), _stream(stream)))
+
+
+def ssmv_conv_history(dims, cache, conv_out, stream=None) -> None:
+    _ck(load_library().ssmv_conv_history(ctypes.byref(dims), ctypes.byref(cache), _ptr(conv_out), _stream(stream)))
 
 
 def ssmv_check(cache, stream=None) -> None:

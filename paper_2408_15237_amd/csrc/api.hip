@@ -5,7 +5,7 @@
 #include <cstdio>
 #include <cstring>
 
-#include "ssmv_internal.h"
+#include "decode_internal.h"
 
 using namespace ssmv;
 
@@ -593,6 +593,291 @@ int ssmv_copy_probe(const void *src, void *dst0, void *dst1, size_t n_bytes, voi
     if (n_bytes == 0 || (n_bytes & 15u) != 0) return fail(SSMV_EINVAL, "n_bytes %zu must be a positive multiple of 16", n_bytes);
     const int hc = launch_copy_probe(src, dst0, dst1, n_bytes, (hipStream_t)hip_stream);
     return hc == 0 ? SSMV_OK : hip_fail(hc, "ssmv_copy_probe");
+}
+
+}  // extern "C"
+
+// ---- plain and beam decoding ---------------------------------------------------------------------------------------------
+
+namespace {
+
+bool aligned_to(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+// a tensor of the I/O type that needs only its elements' alignment
+int check_io(const void *p, int io, const char *name)
+{
+    if (!p) return fail(SSMV_EINVAL, "%s is NULL", name);
+    if (!aligned_to(p, io_bytes(io))) return fail(SSMV_EALIGN, "%s (%p) is not aligned to its elements", name, p);
+    return SSMV_OK;
+}
+
+int check_f32(const void *p, const char *name)
+{
+    if (!p) return fail(SSMV_EINVAL, "%s is NULL", name);
+    if (!aligned_to(p, 4)) return fail(SSMV_EALIGN, "%s (%p) is not 4-byte aligned", name, p);
+    return SSMV_OK;
+}
+
+// 0 = packed
+int check_stride(int64_t *stride, long packed, const char *name)
+{
+    if (*stride == 0) *stride = packed;
+    if (*stride < packed || *stride > (int64_t)1 << 40)
+        return fail(SSMV_EINVAL, "%s %lld: rows of %ld elements would overlap, or it is beyond 2^40", name, (long long)*stride, packed);
+    return SSMV_OK;
+}
+
+int check_io_type(int io)
+{
+    return io == SSMV_F32 || io == SSMV_BF16 ? SSMV_OK : fail(SSMV_EINVAL, "io_dtype %d unknown", io);
+}
+
+int check_rows(int32_t *rows_in, int rows, const int32_t *src_row)
+{
+    if (*rows_in == 0) *rows_in = rows;
+    if (*rows_in < 0) return fail(SSMV_EINVAL, "rows_in %d < 0", *rows_in);
+    if (!src_row && *rows_in < rows) return fail(SSMV_EINVAL, "rows_in %d < %d rows that go out, and no src_row", *rows_in, rows);
+    if (!aligned_to(src_row, 4)) return fail(SSMV_EALIGN, "src_row is not 4-byte aligned");
+    return SSMV_OK;
+}
+
+bool wide(const void *p, int64_t stride, int io) { return aligned16(p) && stride % (io == SSMV_BF16 ? 8 : 4) == 0; }
+
+#define TRY(call) do { const int rc_ = (call); if (rc_ != SSMV_OK) return rc_; } while (0)
+
+}  // namespace
+
+extern "C" {
+
+int ssm_causal_conv(const ssmv_conv_args *args, void *hip_stream)
+{
+    if (!args) return fail(SSMV_EINVAL, "args is NULL");
+    ssmv_conv_args a = *args;
+    TRY(check_io_type(a.io_dtype));
+    if (a.batch < 1 || a.channels < 1 || a.L < 1) return fail(SSMV_EINVAL, "batch %d, channels %d and L %d must be >= 1", a.batch, a.channels, a.L);
+    if (a.act != SSMV_ACT_NONE && a.act != SSMV_ACT_SILU) return fail(SSMV_EINVAL, "act %d unknown", a.act);
+    TRY(check_stride(&a.x_stride, a.channels, "x_stride"));
+    TRY(check_stride(&a.out_stride, a.channels, "out_stride"));
+    TRY(check_rows(&a.rows_in, a.batch, a.src_row));
+    TRY(check_io(a.x, a.io_dtype, "x"));
+    TRY(check_io(a.wgt, a.io_dtype, "wgt"));
+    TRY(check_io(a.out, a.io_dtype, "out"));
+    if (a.bias) TRY(check_io(a.bias, a.io_dtype, "bias"));
+    if (a.conv_in) TRY(check_io(a.conv_in, a.io_dtype, "conv_in"));
+    if (a.conv_out) TRY(check_io(a.conv_out, a.io_dtype, "conv_out"));
+    if (!aligned_to(a.seq_len, 4)) return fail(SSMV_EALIGN, "seq_len is not 4-byte aligned");
+    if (a.out == a.x) return fail(SSMV_EINVAL, "out may not be x: neighbouring tokens read it");
+    if (a.src_row && a.conv_out && a.conv_out == a.conv_in) return fail(SSMV_EINVAL, "conv_out may be conv_in only without src_row");
+    if (a.batch > 65535) return fail(SSMV_EUNSUPPORTED, "batch %d > 65535", a.batch);
+    if ((double)a.batch * a.L * a.channels > 2.0e11) return fail(SSMV_EUNSUPPORTED, "more than 2e11 values");     // 32 bits count the workgroups
+    // a sequence's tiles of at least 8 tokens, counted with 32 bits where every channel has a thread
+    if (((double)a.L / 8 + 1) * a.channels > 2.1e9) return fail(SSMV_EUNSUPPORTED, "a sequence of %d tokens x %d channels: feed it in pieces", a.L, a.channels);
+    CausalConvParams p{};
+    p.x = a.x; p.wgt = a.wgt; p.bias = a.bias; p.conv_in = a.conv_in; p.src_row = a.src_row; p.seq_len = a.seq_len; p.out = a.out; p.conv_out = a.conv_out;
+    p.x_stride = a.x_stride; p.out_stride = a.out_stride;
+    p.batch = a.batch; p.rows_in = a.rows_in; p.C = a.channels; p.L = a.L; p.io = a.io_dtype; p.act = a.act;
+    p.vec = wide(a.x, a.x_stride, p.io) && wide(a.out, a.out_stride, p.io) && wide(a.wgt, 0, p.io) && wide(a.bias, a.channels, p.io) &&
+            wide(a.conv_in, a.channels, p.io) && wide(a.conv_out, a.channels, p.io);
+    const int hc = launch_causal_conv(p, (hipStream_t)hip_stream);
+    return hc == 0 ? SSMV_OK : hip_fail(hc, "ssm_causal_conv");
+}
+
+static int check_scan_sizes(int batch, int channels, int dstate, int L)
+{
+    if (batch < 1 || channels < 1 || L < 1) return fail(SSMV_EINVAL, "batch %d, channels %d and L %d must be >= 1", batch, channels, L);
+    if (dstate != 16 && dstate != 32 && dstate != 64) return fail(SSMV_EUNSUPPORTED, "dstate %d (supported: 16, 32, 64)", dstate);
+    if (batch > 65535) return fail(SSMV_EUNSUPPORTED, "batch %d > 65535", batch);
+    if (channels > (1 << 24) || L > (1 << 30)) return fail(SSMV_EUNSUPPORTED, "more than 2^24 channels or 2^30 tokens");
+    if ((double)batch * L * channels > 2.0e11) return fail(SSMV_EUNSUPPORTED, "more than 2e11 values");           // 32 bits count the workgroups
+    return SSMV_OK;
+}
+
+// [batch][segments][channels] states and sums of steps, each rounded to whole 16 bytes
+static size_t scan_workspace(int batch, int channels, int dstate, int L, int *seg_len, int *seg_count, size_t *dt_at)
+{
+    scan_cut(batch, channels, dstate, L, seg_len, seg_count);
+    if (*seg_count == 1) return *dt_at = 0;
+    const size_t rows = (size_t)batch * *seg_count * channels;
+    *dt_at = rows * dstate * sizeof(float);
+    return *dt_at + (rows * sizeof(float) + 15) / 16 * 16;
+}
+
+int ssm_selective_scan_workspace(int32_t batch, int32_t channels, int32_t dstate, int32_t L, size_t *out_bytes)
+{
+    TRY(check_scan_sizes(batch, channels, dstate, L));
+    if (!out_bytes) return fail(SSMV_EINVAL, "out_bytes is NULL");
+    int len, count;
+    size_t dt_at;
+    *out_bytes = scan_workspace(batch, channels, dstate, L, &len, &count, &dt_at);
+    return SSMV_OK;
+}
+
+int ssm_selective_scan(const ssmv_scan_args *args, void *hip_stream)
+{
+    if (!args) return fail(SSMV_EINVAL, "args is NULL");
+    ssmv_scan_args a = *args;
+    TRY(check_io_type(a.io_dtype));
+    TRY(check_scan_sizes(a.batch, a.channels, a.dstate, a.L));
+    if (a.dt_softplus != 0 && a.dt_softplus != 1) return fail(SSMV_EINVAL, "dt_softplus %d not in {0,1}", a.dt_softplus);
+    TRY(check_stride(&a.x_stride, a.channels, "x_stride"));
+    TRY(check_stride(&a.dt_stride, a.channels, "dt_stride"));
+    TRY(check_stride(&a.b_stride, a.dstate, "b_stride"));
+    TRY(check_stride(&a.c_stride, a.dstate, "c_stride"));
+    TRY(check_stride(&a.z_stride, a.channels, "z_stride"));
+    TRY(check_stride(&a.y_stride, a.channels, "y_stride"));
+    TRY(check_rows(&a.rows_in, a.batch, a.src_row));
+    TRY(check_io(a.x, a.io_dtype, "x"));
+    TRY(check_io(a.dt, a.io_dtype, "dt"));
+    TRY(check_f32(a.Bm, "Bm"));
+    TRY(check_f32(a.Cm, "Cm"));
+    if (a.io_dtype == SSMV_BF16 && (a.b_stride % 2 || a.c_stride % 2)) return fail(SSMV_EALIGN, "rows of B and C must be 4-byte aligned: an even b_stride and c_stride");
+    TRY(check_ptr(a.A, "A"));
+    TRY(check_f32(a.D, "D"));
+    TRY(check_io(a.y_out, a.io_dtype, "y_out"));
+    if (a.z) TRY(check_io(a.z, a.io_dtype, "z"));
+    if (a.dt_bias) TRY(check_f32(a.dt_bias, "dt_bias"));
+    if (a.h_in) TRY(check_ptr(a.h_in, "h_in"));
+    if (a.h_out) TRY(check_ptr(a.h_out, "h_out"));
+    if (!aligned_to(a.seq_len, 4)) return fail(SSMV_EALIGN, "seq_len is not 4-byte aligned");
+    if (a.src_row && a.h_out && a.h_out == a.h_in) return fail(SSMV_EINVAL, "h_out may be h_in only without src_row");
+    ScanParams p{};
+    size_t dt_at;
+    if (scan_workspace(a.batch, a.channels, a.dstate, a.L, &p.seg_len, &p.seg_count, &dt_at) > 0) {
+        TRY(check_ptr(a.workspace, "workspace (this prompt is cut: ssm_selective_scan_workspace)"));
+        p.seg_h = static_cast<float *>(a.workspace);
+        p.seg_dt = p.seg_h + dt_at / sizeof(float);
+    }
+    p.x = a.x; p.dt = a.dt; p.Bm = a.Bm; p.Cm = a.Cm; p.z = a.z; p.dt_bias = a.dt_bias; p.A = a.A; p.D = a.D; p.h_in = a.h_in;
+    p.src_row = a.src_row; p.seq_len = a.seq_len; p.y = a.y_out; p.h_out = a.h_out;
+    p.x_stride = a.x_stride; p.dt_stride = a.dt_stride; p.b_stride = a.b_stride; p.c_stride = a.c_stride; p.z_stride = a.z_stride; p.y_stride = a.y_stride;
+    p.batch = a.batch; p.rows_in = a.rows_in; p.C = a.channels; p.N = a.dstate; p.L = a.L; p.io = a.io_dtype; p.softplus = a.dt_softplus;
+    p.vec = wide(a.x, a.x_stride, p.io) && wide(a.dt, a.dt_stride, p.io) && wide(a.z, a.z_stride, p.io) && wide(a.y_out, a.y_stride, p.io) &&
+            a.channels % 8 == 0;
+    const int hc = launch_selective_scan(p, (hipStream_t)hip_stream);
+    return hc == 0 ? SSMV_OK : hip_fail(hc, "ssm_selective_scan");
+}
+
+int ssm_selective_step(const ssmv_token_args *args, void *hip_stream)
+{
+    if (!args) return fail(SSMV_EINVAL, "args is NULL");
+    ssmv_token_args a = *args;
+    TRY(check_io_type(a.io_dtype));
+    if (a.rows < 1 || a.nheads < 1 || a.headdim < 1 || a.ngroups < 1)
+        return fail(SSMV_EINVAL, "rows %d, nheads %d, headdim %d and ngroups %d must be >= 1", a.rows, a.nheads, a.headdim, a.ngroups);
+    if (a.a_mode != SSMV_A_SCALAR && a.a_mode != SSMV_A_DIAG) return fail(SSMV_EINVAL, "a_mode %d unknown", a.a_mode);
+    if (a.dt_softplus != 0 && a.dt_softplus != 1) return fail(SSMV_EINVAL, "dt_softplus %d not in {0,1}", a.dt_softplus);
+    const bool diag = a.a_mode == SSMV_A_DIAG;
+    if (a.dstate != 16 && a.dstate != 32 && a.dstate != 64 && (diag || (a.dstate != 128 && a.dstate != 256)))
+        return fail(SSMV_EUNSUPPORTED, "dstate %d (supported: 16, 32, 64; scalar mode: 128, 256)", a.dstate);
+    if (diag && (a.headdim != 1 || a.ngroups != 1)) return fail(SSMV_EINVAL, "diag mode needs headdim 1 and ngroups 1 (got %d, %d)", a.headdim, a.ngroups);
+    if (a.nheads % a.ngroups != 0) return fail(SSMV_EINVAL, "nheads %d not a multiple of ngroups %d", a.nheads, a.ngroups);
+    if ((double)a.nheads * a.headdim * a.dstate >= 1.0e9) return fail(SSMV_EUNSUPPORTED, "a state of 1e9 values or more");
+    if (a.rows > 65535) return fail(SSMV_EUNSUPPORTED, "rows %d > 65535", a.rows);
+    const long Cx = (long)a.nheads * a.headdim, GN = (long)a.ngroups * a.dstate;
+    TRY(check_stride(&a.x_stride, Cx, "x_stride"));
+    TRY(check_stride(&a.dt_stride, a.nheads, "dt_stride"));
+    TRY(check_stride(&a.b_stride, GN, "b_stride"));
+    TRY(check_stride(&a.c_stride, GN, "c_stride"));
+    TRY(check_stride(&a.z_stride, Cx, "z_stride"));
+    TRY(check_stride(&a.y_stride, Cx, "y_stride"));
+    TRY(check_rows(&a.rows_in, a.rows, a.src_row));
+    TRY(check_io(a.x, a.io_dtype, "x"));
+    TRY(check_io(a.dt, a.io_dtype, "dt"));
+    TRY(check_f32(a.Bm, "Bm"));
+    TRY(check_f32(a.Cm, "Cm"));
+    if (a.io_dtype == SSMV_BF16 && (a.b_stride % 2 || a.c_stride % 2)) return fail(SSMV_EALIGN, "rows of B and C must be 4-byte aligned: an even b_stride and c_stride");
+    if (diag) TRY(check_ptr(a.A, "A"));
+    else TRY(check_f32(a.A, "A"));
+    TRY(check_f32(a.D, "D"));
+    TRY(check_io(a.y_out, a.io_dtype, "y_out"));
+    TRY(check_ptr(a.h_out, "h_out"));
+    if (a.h_in) TRY(check_ptr(a.h_in, "h_in"));
+    if (a.z) TRY(check_io(a.z, a.io_dtype, "z"));
+    if (a.dt_bias) TRY(check_f32(a.dt_bias, "dt_bias"));
+    if (a.src_row && a.h_out == a.h_in) return fail(SSMV_EINVAL, "h_out may be h_in only without src_row");
+    TokenParams p{};
+    p.x = a.x; p.dt = a.dt; p.Bm = a.Bm; p.Cm = a.Cm; p.z = a.z; p.dt_bias = a.dt_bias; p.A = a.A; p.D = a.D; p.h_in = a.h_in; p.src_row = a.src_row;
+    p.y = a.y_out; p.h_out = a.h_out;
+    p.x_stride = a.x_stride; p.dt_stride = a.dt_stride; p.b_stride = a.b_stride; p.c_stride = a.c_stride; p.z_stride = a.z_stride; p.y_stride = a.y_stride;
+    p.rows = a.rows; p.rows_in = a.rows_in; p.H = a.nheads; p.P = a.headdim; p.N = a.dstate; p.G = a.ngroups; p.io = a.io_dtype; p.diag = diag;
+    p.softplus = a.dt_softplus;
+    const int hc = launch_selective_step(p, (hipStream_t)hip_stream);
+    return hc == 0 ? SSMV_OK : hip_fail(hc, "ssm_selective_step");
+}
+
+static int check_beam_sizes(int batch, int beams_in, int beams_out, int vocab)
+{
+    if (batch < 1 || beams_in < 1 || beams_out < 1 || vocab < 1)
+        return fail(SSMV_EINVAL, "batch %d, beams_in %d, beams_out %d and vocab %d must be >= 1", batch, beams_in, beams_out, vocab);
+    if (beams_in > SSMV_BEAMS_MAX || beams_out > SSMV_BEAMS_MAX)
+        return fail(SSMV_EUNSUPPORTED, "beams_in %d, beams_out %d: at most %d", beams_in, beams_out, SSMV_BEAMS_MAX);
+    if (beams_out > (long)beams_in * vocab) return fail(SSMV_EINVAL, "beams_out %d of %ld candidates", beams_out, (long)beams_in * vocab);
+    if (vocab > 1 << 24) return fail(SSMV_EUNSUPPORTED, "vocab %d > 2^24", vocab);
+    if ((long)batch * beams_in > 65535) return fail(SSMV_EUNSUPPORTED, "more than 65535 rows");
+    return SSMV_OK;
+}
+
+// keys [row][piece][keep], then sums [row][piece]
+static size_t beam_layout(int batch, int beams_in, int beams_out, int vocab, int *pieces, int *keep, size_t *sums_at)
+{
+    const int rows = batch * beams_in;
+    *pieces = beam_pieces(rows, vocab);
+    *keep = beams_out < vocab ? beams_out : vocab;
+    *sums_at = ((size_t)rows * *pieces * *keep * sizeof(unsigned long long) + 15) / 16 * 16;
+    return *sums_at + ((size_t)rows * *pieces * sizeof(float2) + 15) / 16 * 16;
+}
+
+int ssmv_beam_workspace(int32_t batch, int32_t beams_in, int32_t beams_out, int32_t vocab, size_t *out_bytes)
+{
+    TRY(check_beam_sizes(batch, beams_in, beams_out, vocab));
+    if (!out_bytes) return fail(SSMV_EINVAL, "out_bytes is NULL");
+    int pieces, keep;
+    size_t at;
+    *out_bytes = beam_layout(batch, beams_in, beams_out, vocab, &pieces, &keep, &at);
+    return SSMV_OK;
+}
+
+int ssmv_beam_select(const ssmv_beam_args *args, void *hip_stream)
+{
+    if (!args) return fail(SSMV_EINVAL, "args is NULL");
+    ssmv_beam_args a = *args;
+    TRY(check_io_type(a.io_dtype));
+    TRY(check_beam_sizes(a.batch, a.beams_in, a.beams_out, a.vocab));
+    TRY(check_stride(&a.row_stride, a.vocab, "row_stride"));
+    if (a.eos < -1 || a.eos >= a.vocab) return fail(SSMV_EINVAL, "eos %d outside [-1, vocab = %d)", a.eos, a.vocab);
+    if (a.done && a.eos < 0) return fail(SSMV_EINVAL, "finished rows need an eos token");
+    TRY(check_io(a.logits, a.io_dtype, "logits"));
+    TRY(check_f32(a.scores, "scores"));
+    TRY(check_f32(a.parent, "parent"));
+    TRY(check_f32(a.token, "token"));
+    TRY(check_f32(a.scores_out, "scores_out"));
+    if (a.done) TRY(check_f32(a.done, "done"));
+    if (a.done_out) TRY(check_f32(a.done_out, "done_out"));
+    if (a.scores_out == a.scores || (a.done_out && a.done_out == a.done)) return fail(SSMV_EINVAL, "scores_out and done_out may not be scores and done");
+    TRY(check_ptr(a.workspace, "workspace"));
+    BeamParams p{};
+    p.logits = a.logits; p.scores = a.scores; p.done = a.done; p.parent = a.parent; p.token = a.token; p.scores_out = a.scores_out; p.done_out = a.done_out;
+    p.row_stride = a.row_stride;
+    p.batch = a.batch; p.beams_in = a.beams_in; p.beams_out = a.beams_out; p.V = a.vocab; p.io = a.io_dtype; p.eos = a.eos;
+    p.vec = wide(a.logits, a.row_stride, p.io);
+    size_t sums_at;
+    beam_layout(a.batch, a.beams_in, a.beams_out, a.vocab, &p.pieces, &p.keep, &sums_at);
+    p.keys = static_cast<unsigned long long *>(a.workspace);
+    p.sums = reinterpret_cast<float2 *>(static_cast<char *>(a.workspace) + sums_at);
+    const int hc = launch_beam_select(p, (hipStream_t)hip_stream);
+    return hc == 0 ? SSMV_OK : hip_fail(hc, "ssmv_beam_select");
+}
+
+int ssmv_conv_history(const ssmv_dims *d, const ssmv_cache *c, void *conv_out, void *hip_stream)
+{
+    TRY(check_dims(d));
+    TRY(check_cache(c));
+    TRY(check_io(conv_out, d->io_dtype, "conv_out"));
+    ConvHistoryParams p{};
+    p.batch = d->batch; p.R = d->ring_len; p.Cx = d->conv_channels; p.io = d->io_dtype;
+    p.ring = c->conv_ring; p.conv_head = c->conv_head; p.out = conv_out;
+    const int hc = launch_conv_history(p, (hipStream_t)hip_stream);
+    return hc == 0 ? SSMV_OK : hip_fail(hc, "ssmv_conv_history");
 }
 
 }  // extern "C"

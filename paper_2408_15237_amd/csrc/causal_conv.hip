@@ -1,0 +1,162 @@
+// The causal depthwise convolution of width 4 from a history of raw inputs to the newest one, over a prompt or one token of every row,
+// and the conv part of a cache's state.
+#include "decode_internal.h"
+
+namespace ssmv {
+namespace {
+
+constexpr int W = SSMV_CONV_WIDTH;
+
+// VEC elements of one token row: 16 bytes, or one element where the tensors do not allow more
+template <int IO, int VEC>
+struct Chunk {
+    using Vec = IoVec<IO>;
+    static __device__ __forceinline__ uint4 zero() { return make_uint4(0, 0, 0, 0); }
+    static __device__ __forceinline__ uint4 load(const void *base, size_t idx)
+    {
+        if constexpr (VEC > 1) return Vec::load_raw(base, idx);
+        else return make_uint4(Vec::load_raw1(base, idx), 0, 0, 0);
+    }
+    static __device__ __forceinline__ void store(void *base, size_t idx, uint4 r)
+    {
+        if constexpr (VEC > 1) Vec::store_raw(base, idx, r);
+        else Vec::store_raw1(base, idx, r.x);
+    }
+    static __device__ __forceinline__ void decode(uint4 r, float (&v)[VEC])
+    {
+        if constexpr (VEC > 1) Vec::decode(r, v);
+        else v[0] = Vec::decode1(r.x);
+    }
+    static __device__ __forceinline__ uint4 encode(const float (&v)[VEC])
+    {
+        if constexpr (VEC > 1) return Vec::encode(v);
+        else if constexpr (IO == SSMV_BF16) return make_uint4(f32_to_bf16_bits(v[0]), 0, 0, 0);
+        else return make_uint4(__float_as_uint(v[0]), 0, 0, 0);
+    }
+};
+
+// A thread owns VEC adjacent channels of T tokens: it requests its tokens and the three before them together, and slides over
+// them in registers.  The three are those of the thread of the tokens before, out of the L2; the first tokens take the history, and
+// their thread also leaves the newest three inputs, so that conv_out may be conv_in.
+template <int IO, int VEC, int T>
+__global__ __launch_bounds__(256) void causal_conv_kernel(const CausalConvParams p, unsigned chunks, unsigned items)
+{
+    using Ch = Chunk<IO, VEC>;
+    const unsigned lin = xcd_contiguous(blockIdx.y * gridDim.x + blockIdx.x, gridDim.x * gridDim.y);
+    const unsigned b = lin / gridDim.x, item = (lin - b * gridDim.x) * 256 + threadIdx.x;
+    if (item >= items) return;
+    const unsigned tile = item / chunks, c0 = (item - tile * chunks) * VEC;
+    const int len = p.seq_len ? min(max(p.seq_len[b], 0), p.L) : p.L;
+    const int t0 = (int)tile * T;
+    const bool first = t0 == 0;
+    if (t0 >= len && !first) return;
+
+    const size_t row0 = (size_t)b * p.L;                       // the sequence's tokens
+    auto x_at = [&](int t) { return Ch::load(p.x, (row0 + t) * p.x_stride + c0); };
+    uint4 raw[W - 1 + T];
+    uint4 hist[W - 1];
+    if (first) {
+        const int src = p.src_row ? p.src_row[b] : (int)b;
+        const bool have = p.conv_in && (unsigned)src < (unsigned)p.rows_in;
+#pragma unroll
+        for (int i = 0; i < W - 1; ++i) hist[i] = have ? Ch::load(p.conv_in, ((size_t)src * (W - 1) + i) * p.C + c0) : Ch::zero();
+#pragma unroll
+        for (int i = 0; i < W - 1; ++i) raw[i] = hist[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < W - 1; ++i) raw[i] = x_at(t0 - (W - 1) + i);
+    }
+    if (len > 0) {
+        // tokens behind the last one: the last one again, dropped below
+#pragma unroll
+        for (int i = 0; i < T; ++i) raw[W - 1 + i] = x_at(min(t0 + i, len - 1));
+        float w[VEC][W], bias[VEC], v[W][VEC];
+        if constexpr (VEC > 1) {
+#pragma unroll
+            for (int i = 0; i < W; ++i) {                      // 4 VEC adjacent weights: W vectors
+                float t[VEC];
+                Ch::decode(Ch::load(p.wgt, (size_t)c0 * W + i * VEC), t);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) w[(i * VEC + j) / W][(i * VEC + j) % W] = t[j];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < W; ++i) w[0][i] = load_io(p.wgt, (size_t)c0 * W + i, IO);
+        }
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) bias[j] = 0.f;
+        if (p.bias) Ch::decode(Ch::load(p.bias, c0), bias);
+#pragma unroll
+        for (int i = 0; i < W - 1; ++i) Ch::decode(raw[i], v[i]);
+#pragma unroll
+        for (int i = 0; i < T; ++i) {
+            Ch::decode(raw[W - 1 + i], v[(W - 1 + i) % W]);
+            if (t0 + i < len) {
+                float o[VEC];
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    o[j] = bias[j];
+#pragma unroll
+                    for (int k = 0; k < W; ++k) o[j] = fmaf(w[j][k], v[(i + k) % W][j], o[j]);
+                    if (p.act == SSMV_ACT_SILU) o[j] = silu_fast(o[j]);
+                }
+                Ch::store(p.out, (row0 + t0 + i) * p.out_stride + c0, Ch::encode(o));
+            }
+        }
+    }
+    if (first && p.conv_out) {
+#pragma unroll
+        for (int i = 0; i < W - 1; ++i) {
+            const int t = len - (W - 1) + i;
+            uint4 r;
+            if (t >= 0) r = x_at(t);
+            else r = len == 0 ? hist[i] : len == 1 ? hist[i + 1 < W - 1 ? i + 1 : i] : hist[W - 2];       // len + i of the history
+            Ch::store(p.conv_out, ((size_t)b * (W - 1) + i) * p.C + c0, r);
+        }
+    }
+}
+
+template <int IO, int VEC>
+int launch(const CausalConvParams &p, hipStream_t stream)
+{
+    const unsigned chunks = (unsigned)((p.C + VEC - 1) / VEC);
+    auto go = [&](auto kernel, int T) {
+        const size_t items = (size_t)((p.L + T - 1) / T) * chunks;
+        if (items > 0x7fffff00u || p.batch > 65535) return (int)hipErrorInvalidValue;      // refused by the host's checks
+        const dim3 grid((unsigned)((items + 255) / 256), (unsigned)p.batch);
+        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, p, chunks, (unsigned)items);
+        return (int)hipGetLastError();
+    };
+    if (p.L == 1) return go(causal_conv_kernel<IO, VEC, 1>, 1);
+    return go(causal_conv_kernel<IO, VEC, 8>, 8);
+}
+
+// a thread per element of conv_out
+__global__ __launch_bounds__(256) void conv_history_kernel(const ConvHistoryParams p)
+{
+    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= (size_t)p.batch * (W - 1) * p.Cx) return;
+    const size_t row = i / p.Cx;
+    const unsigned c = (unsigned)(i - row * p.Cx), b = (unsigned)(row / (W - 1)), k = (unsigned)(row - (size_t)b * (W - 1));
+    const size_t at = ((size_t)b * p.R + ((p.conv_head[b] - (W - 2) + (int)k) & (p.R - 1))) * p.Cx + c;
+    if (p.io == SSMV_BF16) static_cast<uint16_t *>(p.out)[i] = static_cast<const uint16_t *>(p.ring)[at];
+    else static_cast<uint32_t *>(p.out)[i] = static_cast<const uint32_t *>(p.ring)[at];
+}
+
+}  // namespace
+
+int launch_causal_conv(const CausalConvParams &p, hipStream_t stream)
+{
+    constexpr int EB = IoVec<SSMV_BF16>::EV, EF = IoVec<SSMV_F32>::EV;
+    if (p.io == SSMV_BF16) return p.vec && p.C % EB == 0 ? launch<SSMV_BF16, EB>(p, stream) : launch<SSMV_BF16, 1>(p, stream);
+    return p.vec && p.C % EF == 0 ? launch<SSMV_F32, EF>(p, stream) : launch<SSMV_F32, 1>(p, stream);
+}
+
+int launch_conv_history(const ConvHistoryParams &p, hipStream_t stream)
+{
+    const size_t n = (size_t)p.batch * (W - 1) * p.Cx;
+    hipLaunchKernelGGL(conv_history_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, stream, p);
+    return (int)hipGetLastError();
+}
+
+}  // namespace ssmv
