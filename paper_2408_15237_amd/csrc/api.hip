@@ -693,11 +693,10 @@ static int check_scan_sizes(int batch, int channels, int dstate, int L)
 }
 
 // [batch][segments][channels] states and sums of steps, each rounded to whole 16 bytes
-static size_t scan_workspace(int batch, int channels, int dstate, int L, int *seg_len, int *seg_count, size_t *dt_at)
+static size_t scan_workspace(int batch, int channels, const ScanPlan &plan, int dstate, size_t *dt_at)
 {
-    scan_cut(batch, channels, dstate, L, seg_len, seg_count);
-    if (*seg_count == 1) return *dt_at = 0;
-    const size_t rows = (size_t)batch * *seg_count * channels;
+    if (plan.seg_count == 1) return *dt_at = 0;
+    const size_t rows = (size_t)batch * plan.seg_count * channels;
     *dt_at = rows * dstate * sizeof(float);
     return *dt_at + (rows * sizeof(float) + 15) / 16 * 16;
 }
@@ -706,9 +705,8 @@ int ssm_selective_scan_workspace(int32_t batch, int32_t channels, int32_t dstate
 {
     TRY(check_scan_sizes(batch, channels, dstate, L));
     if (!out_bytes) return fail(SSMV_EINVAL, "out_bytes is NULL");
-    int len, count;
     size_t dt_at;
-    *out_bytes = scan_workspace(batch, channels, dstate, L, &len, &count, &dt_at);
+    *out_bytes = scan_workspace(batch, channels, scan_plan(batch, channels, dstate, L), dstate, &dt_at);
     return SSMV_OK;
 }
 
@@ -742,7 +740,9 @@ int ssm_selective_scan(const ssmv_scan_args *args, void *hip_stream)
     if (a.src_row && a.h_out && a.h_out == a.h_in) return fail(SSMV_EINVAL, "h_out may be h_in only without src_row");
     ScanParams p{};
     size_t dt_at;
-    if (scan_workspace(a.batch, a.channels, a.dstate, a.L, &p.seg_len, &p.seg_count, &dt_at) > 0) {
+    const ScanPlan plan = scan_plan(a.batch, a.channels, a.dstate, a.L);
+    p.channels_wg = plan.channels; p.seg_len = plan.seg_len; p.seg_count = plan.seg_count;
+    if (scan_workspace(a.batch, a.channels, plan, a.dstate, &dt_at) > 0) {
         TRY(check_ptr(a.workspace, "workspace (this prompt is cut: ssm_selective_scan_workspace)"));
         p.seg_h = static_cast<float *>(a.workspace);
         p.seg_dt = p.seg_h + dt_at / sizeof(float);
@@ -752,7 +752,7 @@ int ssm_selective_scan(const ssmv_scan_args *args, void *hip_stream)
     p.x_stride = a.x_stride; p.dt_stride = a.dt_stride; p.b_stride = a.b_stride; p.c_stride = a.c_stride; p.z_stride = a.z_stride; p.y_stride = a.y_stride;
     p.batch = a.batch; p.rows_in = a.rows_in; p.C = a.channels; p.N = a.dstate; p.L = a.L; p.io = a.io_dtype; p.softplus = a.dt_softplus;
     p.vec = wide(a.x, a.x_stride, p.io) && wide(a.dt, a.dt_stride, p.io) && wide(a.z, a.z_stride, p.io) && wide(a.y_out, a.y_stride, p.io) &&
-            a.channels % 8 == 0;
+            a.channels % 4 == 0;
     const int hc = launch_selective_scan(p, (hipStream_t)hip_stream);
     return hc == 0 ? SSMV_OK : hip_fail(hc, "ssm_selective_scan");
 }

@@ -6,6 +6,15 @@
 
 namespace ssmv {
 
+// log(1 + e^v) for all v: max(v, 0) + log(1 + t), t = e^-|v|; what the rounding of w = 1 + t loses of a small t is given back, as
+// log(w + r) = log(w) + r to within 2^-25 for w in [1, 2].  Within 2e-7 of the exact value for every t, where the plain log(1 + t) is
+// off by 4e-6 at t = 2^-6; no select and no series.
+__device__ __forceinline__ float softplus_exact(float v)
+{
+    const float t = __builtin_amdgcn_exp2f(-1.4426950408889634f * fabsf(v)), w = 1.f + t;
+    return fmaf(__builtin_amdgcn_logf(w), 0.69314718055994531f, t - (w - 1.f)) + fmaxf(v, 0.f);
+}
+
 struct CausalConvParams {
     const void *x, *wgt, *bias, *conv_in;
     const int32_t *src_row, *seq_len;
@@ -24,6 +33,7 @@ struct ScanParams {
     size_t x_stride, dt_stride, b_stride, c_stride, z_stride, y_stride;
     int batch, rows_in, C, N, L, io, softplus;
     int vec;                 // 1: 16-byte accesses of x, dt, z and y
+    int channels_wg;         // channels of a workgroup: 64, 32, 16 (not with N = 64)
     int seg_len, seg_count;  // a cut prompt: tokens of a segment, segments of the longest prompt; seg_count 1: not cut
     float *seg_h;            // [batch][seg_count][C][N] end states of the segments, the first slice of each sequence; see selective_scan.hip
     float *seg_dt;           // [batch][seg_count][C]    their sums of step sizes
@@ -64,13 +74,43 @@ struct ConvHistoryParams {
 
 // ---- how a prompt is cut and a row of logits divided: the workspaces follow from it --------------------------------------
 
-constexpr int kScanTile = 32;        // tokens that a workgroup of the scan takes at a time
+constexpr int kScanTile = 64;        // tokens of a segment: a multiple of this
 
-// Tokens of a segment and segments of the longest prompt.
-inline void scan_cut(int batch, int C, int N, int L, int *seg_len, int *seg_count)
+struct ScanPlan {
+    int channels;            // of a workgroup: 64, 32 or 16 (N < 64)
+    int seg_len, seg_count;  // tokens of a segment, segments of the longest prompt
+};
+
+// Which width of workgroup, and how many segments: the least time by a model of the kernel, whose constants were measured.  Of a
+// token a workgroup that has a compute unit to itself takes lone = 15 + N ns (16 channels), 18 + 1.6 N (32), 35 + 2.6 N (64); a compute
+// unit with k of them takes k times 14 + 0.75 N, 15 + 1.3 N, 22 + 2.5 N where that is more.  A cut prompt costs a pass over all
+// segments but the last that forms their end states (0.65 of a full pass), and 5 us.
+// (us, N = 16, 2048 tokens, 64 / 32 / 16 channels: 1 x 8192 152 / 91 / 105; 1 x 1536 151 / 81 / 65, in 8 segments 42 / 37 / 37;
+//  8 x 5120 380 / 360 / 445; 16 x 8192 953 / 1088 / 1385, and 1606 / 1825 / 2248 in 8 segments.)
+inline ScanPlan scan_plan(int batch, int C, int N, int L)
 {
-    *seg_len = L;
-    *seg_count = 1;
+    const int tiles = (L + kScanTile - 1) / kScanTile;
+    ScanPlan best{64, L, 1};
+    double least = 1e30;
+    for (int w = 64; w >= (N < 64 ? 16 : 32); w /= 2) {
+        const double lone = w == 64 ? 35 + 2.6 * N : w == 32 ? 18 + 1.6 * N : 15 + 1.0 * N;
+        const double busy = w == 64 ? 22 + 2.5 * N : w == 32 ? 15 + 1.3 * N : 14 + 0.75 * N;
+        const double groups = (double)batch * ((C + w - 1) / w);
+        for (int want = 1; want <= 16 && want <= tiles; ++want) {
+            const int len = (tiles + want - 1) / want * kScanTile, count = (L + len - 1) / len;
+            if (count != want) continue;
+            auto pass = [&](double g) {
+                const double k = (double)(long)((g + 255) / 256) * busy;
+                return 1e-3 * (count > 1 ? len : L) * (k > lone ? k : lone);
+            };
+            const double us = pass(groups * count) + (count > 1 ? 0.65 * pass(groups * (count - 1)) + 5.0 : 0.0);
+            if (us < least) {
+                least = us;
+                best = ScanPlan{w, count > 1 ? len : L, count};
+            }
+        }
+    }
+    return best;
 }
 
 constexpr int kBeamPiece = 8192;     // logits that a workgroup of the selection takes

@@ -1,4 +1,7 @@
 // A prompt through the recurrence with a decay per channel and state index, from state to state.
+#include <type_traits>
+#include <utility>
+
 #include "decode_internal.h"
 
 namespace ssmv {
@@ -6,24 +9,6 @@ namespace {
 
 typedef float v4 __attribute__((ext_vector_type(4)));
 
-constexpr int kChannels = 64;            // channels of a workgroup: a lane each
-constexpr int T = kScanTile;
-
-// log(1 + e^v) for all v: max(v, 0) + log1p(t), t = e^-|v|, and log1p(t) = 2 atanh(s), s = t / (2 + t) <= 1/3, by its series up to s^13
-// (what is left out is under 2^-25 of it).  No select, and no 1 + t that would lose the low bits of a small t.
-__device__ __forceinline__ float softplus_series(float v)
-{
-    const float t = __builtin_amdgcn_exp2f(-1.4426950408889634f * fabsf(v));
-    const float s = t * __builtin_amdgcn_rcpf(2.f + t), q = s * s;
-    float f = 2.f / 13.f;
-    f = fmaf(f, q, 2.f / 11.f);
-    f = fmaf(f, q, 2.f / 9.f);
-    f = fmaf(f, q, 2.f / 7.f);
-    f = fmaf(f, q, 2.f / 5.f);
-    f = fmaf(f, q, 2.f / 3.f);
-    f = fmaf(f, q, 2.f);
-    return fmaf(s, f, fmaxf(v, 0.f));
-}
 
 // CH values of adjacent channels as stored; behind the last channel zeros
 template <int IO, int CH>
@@ -98,153 +83,288 @@ __device__ __forceinline__ void store_piece(void *base, size_t idx, const float 
     }
 }
 
-// S state indices of a token's B or C, the same for all lanes: scalar loads
-template <int IO, int S>
-struct Coef {
-    static constexpr int NW = IO == SSMV_BF16 ? S / 2 : S;
-    uint32_t w[NW];
-    __device__ __forceinline__ void load(const void *row)
-    {
-        const auto *s = (const __attribute__((address_space(4))) uint32_t *)(uintptr_t)row;
-#pragma unroll
-        for (int i = 0; i < NW; ++i) w[i] = s[i];
-    }
-    __device__ __forceinline__ float get(int i) const
-    {
-        if constexpr (IO == SSMV_BF16) return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
-        else return __uint_as_float(w[i]);
-    }
-};
-
-// A workgroup takes 64 channels of a sequence, T tokens at a time: a lane per channel, a wave per S state indices, so that B and C of
-// a token are wave-uniform (scalar registers) and a lane's state stays in registers from the first token to the last.  Around the
-// recurrence every thread owns CH adjacent channels of one token of the tile: it prepares (dt', dt' x) for the waves, and sums their
-// partial outputs, adds the skip, gates and stores.  Both change hands in LDS.
-template <int IO, int N, int S, bool VEC>
-__global__ __launch_bounds__(64 * (N / S)) void selective_scan_kernel(const ScanParams p)
+// the value that lane k of each 16 holds: an operand modifier of the multiplication that takes it
+template <int K>
+__device__ __forceinline__ float row_get(float v)
 {
-    constexpr int NW = N / S, THREADS = 64 * NW, CH = T * kChannels / THREADS, PER_ROW = kChannels / CH, U = 8;
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x150 + K, 0xf, 0xf, true));
+}
+
+template <typename F, int... I>
+__device__ __forceinline__ void unroll(F &&f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
+
+template <int S>
+__device__ __forceinline__ void load_state(const float *from, float (&to)[S])
+{
+    if constexpr (S >= 4) {
+#pragma unroll
+        for (int i = 0; i < S; i += 4) {
+            const v4 t = *reinterpret_cast<const v4 *>(from + i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) to[i + j] = t[j];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < S; ++i) to[i] = from[i];
+    }
+}
+template <int S>
+__device__ __forceinline__ void store_state(float *to, const float (&from)[S])
+{
+    if constexpr (S >= 4) {
+#pragma unroll
+        for (int i = 0; i < S; i += 4) *reinterpret_cast<v4 *>(to + i) = v4{from[i], from[i + 1], from[i + 2], from[i + 3]};
+    } else {
+#pragma unroll
+        for (int i = 0; i < S; ++i) to[i] = from[i];
+    }
+}
+
+// (a, b) -> (rows 0, 1 of a | rows 0, 1 of b), (rows 2, 3 of a | rows 2, 3 of b), summed
+__device__ __forceinline__ float fold32(float a, float b)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// the same of rows 0 and 1, and of rows 2 and 3
+__device__ __forceinline__ float fold16(float a, float b)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+constexpr int kScanWaves = 4, kHelpWaves = 4;
+
+// A workgroup takes CHW channels of a sequence, T tokens at a time.  Four of its waves scan: a lane per channel and S of the N state
+// indices, which stay in registers from the first token to the last; with fewer than 64 channels the 64 / CHW parts of a wave take
+// other indices of the same channels.  Four waves help: each of their threads owns CH adjacent channels of one token of a
+// tile, prepares (dt', dt' x) of the tile ahead of the scan, and of the tile behind it sums the partial outputs, adds the skip, gates
+// and stores, so that a tile's three stages run side by side and one barrier a tile is enough.  Everything changes hands in LDS.
+// B of a token is a broadcast operand: 16 / S tokens' worth sit in the lanes of every 16 of a register.
+// OUT false: only the state at the segment's end and the sum of its steps, of all segments but the last.
+template <int IO, int N, int CHW, bool VEC, bool OUT>
+__global__ __launch_bounds__(64 * (kScanWaves + kHelpWaves)) __attribute__((amdgpu_waves_per_eu(4)))
+void selective_scan_kernel(const ScanParams p)
+{
+    constexpr int S = N * CHW / (64 * kScanWaves), R = 64 / CHW;                  // states of a lane; parts of a wave
+    constexpr int CH = 4, T = 64 * kHelpWaves * CH / CHW, PER_ROW = CHW / CH, U = S >= 4 ? 4 : 8;
+    constexpr int BC = 2 * T * N / (64 * kHelpWaves);                             // values of B and C that a thread fetches: of one token, adjacent
+    constexpr int TB = S >= 16 ? 1 : 16 / S;                                      // tokens whose B share a register
     constexpr float LOG2E = 1.4426950408889634f;
-    __shared__ __attribute__((aligned(16))) float2 sIn[T][kChannels];             // (dt', dt' x)
-    __shared__ __attribute__((aligned(16))) float sY[NW][T][kChannels];
+    static_assert(S >= 1 && T % U == 0 && kScanTile % T == 0, "tile");
+    __shared__ __attribute__((aligned(16))) float2 sIn[2][T][CHW];                // (dt', dt' x)
+    __shared__ __attribute__((aligned(16))) float sB[2][T][N];
+    __shared__ __attribute__((aligned(16))) float sC[2][OUT ? T : 1][N];
+    __shared__ __attribute__((aligned(16))) float sY[2][kScanWaves][OUT ? T : 1][CHW];
 
-    const unsigned tid = threadIdx.x, lane = tid & 63u;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const unsigned blocks = gridDim.x;
-    const unsigned lin = xcd_contiguous(blockIdx.y * blocks + blockIdx.x, blocks * gridDim.y);
-    const int b = __builtin_amdgcn_readfirstlane(lin / blocks), c0 = (int)(lin - (unsigned)b * blocks) * kChannels;
-    const int len = p.seq_len ? min(max(p.seq_len[b], 0), p.L) : p.L;
+    const unsigned lane = threadIdx.x & 63u;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned lin = xcd_contiguous(blockIdx.x, gridDim.x);                   // channels next to each other share cache lines
+    const int c0 = (int)lin * CHW, seg = blockIdx.y, b = blockIdx.z;
+    const int all = p.seq_len ? min(max(p.seq_len[b], 0), p.L) : p.L;
+    const int from = seg * p.seg_len, len = min(all, from + p.seg_len);           // the segment's tokens
+    const bool last = len == all;
+    if (OUT ? (seg > 0 && from >= all) : (seg > 0 && last)) return;
+    const size_t slice = (size_t)p.C * N, tok0 = (size_t)b * p.L;
+    float *seg_h = p.seg_h + (size_t)b * p.seg_count * slice;                     // the sequence's end states; the last place: where it starts
 
-    // the lane's part of the state
-    const int c = min(c0 + (int)lane, p.C - 1);                                   // lanes past the last channel double it and store nothing
-    const bool have = c0 + (int)lane < p.C;
-    const int src = p.src_row ? p.src_row[b] : b;
-    const size_t own = (size_t)c * N + wave * S;
-    float h[S], a[S];
+    if (wave < kScanWaves) {
+        const int c = min(c0 + (int)(lane % CHW), p.C - 1);                       // lanes past the last channel double it and store nothing
+        const bool have = c0 + (int)(lane % CHW) < p.C;
+        const int n0 = (wave * R + (int)lane / CHW) * S;                          // the lane's state indices
+        const size_t own = (size_t)c * N + n0;
+        const float *seg_dt = p.seg_dt + (size_t)b * p.seg_count * p.C;
+        float h[S], a[S];
+        load_state<S>(p.A + own, a);
 #pragma unroll
-    for (int i = 0; i < S; i += 4) {
-        const v4 t = *reinterpret_cast<const v4 *>(p.A + own + i) * LOG2E;
-        v4 s = v4{0.f, 0.f, 0.f, 0.f};
-        if (p.h_in && (unsigned)src < (unsigned)p.rows_in) s = *reinterpret_cast<const v4 *>(p.h_in + (size_t)src * p.C * N + own + i);
+        for (int i = 0; i < S; ++i) { a[i] *= LOG2E; h[i] = 0.f; }
+        if (seg == 0) {
+            const int src = p.src_row ? p.src_row[b] : b;
+            if (OUT && p.seg_count > 1) load_state<S>(seg_h + (p.seg_count - 1) * slice + own, h);    // h_out may be h_in, and its writer another workgroup
+            else if (p.h_in && (unsigned)src < (unsigned)p.rows_in) load_state<S>(p.h_in + (size_t)src * slice + own, h);
+            if (!OUT && have) store_state<S>(seg_h + (p.seg_count - 1) * slice + own, h);
+        } else if (OUT) {
+            load_state<S>(seg_h + own, h);
+            for (int j = 1; j < seg; ++j) {
+                float e[S];
+                load_state<S>(seg_h + j * slice + own, e);
+                const float sum = seg_dt[(size_t)j * p.C + c];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) { a[i + j] = t[j]; h[i + j] = s[j]; }
+                for (int i = 0; i < S; ++i) h[i] = fmaf(h[i], __builtin_amdgcn_exp2f(a[i] * sum), e[i]);
+            }
+        }
+        if (!OUT && last) return;                                                 // the whole workgroup: the helpers below, too
+        float sum = 0.f;                                                          // of the lane's steps
+        __syncthreads();
+        for (int t0 = from, buf = 0; t0 < len; t0 += T, buf ^= 1) {
+            const int n = min(len - t0, T);
+            for (int u0 = 0; u0 < n; u0 += U) {
+                float2 in[U];
+                float y[U], coef[S >= 16 ? U : (U + TB - 1) / TB];
+#pragma unroll
+                for (int u = 0; u < U; ++u) in[u] = sIn[buf][u0 + u][lane % CHW];
+#pragma unroll
+                for (int u = 0; u < U; u += TB)
+                    coef[u / TB] = sB[buf][u0 + u + (S >= 16 ? 0 : ((int)lane % 16 / S) % U)][n0 + (int)lane % (S >= 16 ? 16 : S)];
+                unroll([&](auto uu) {
+                    constexpr int u = decltype(uu)::value;
+                    float C[S];
+                    y[u] = 0.f;
+                    if constexpr (OUT) load_state<S>(&sC[buf][u0 + u][n0], C);
+                    unroll([&](auto ii) {
+                        constexpr int i = decltype(ii)::value;
+                        h[i] = fmaf(h[i], __builtin_amdgcn_exp2f(a[i] * in[u].x), row_get<S >= 16 ? i : u % TB * S + i>(coef[u / TB]) * in[u].y);
+                        if constexpr (OUT) y[u] = fmaf(C[i], h[i], y[u]);
+                    }, std::make_integer_sequence<int, S>{});
+                    if constexpr (!OUT) sum += in[u].x;
+                }, std::make_integer_sequence<int, U>{});
+                if constexpr (OUT) {
+#pragma unroll
+                    for (int u = 0; u < U; u += R) {                              // part r of the wave ends up with token u + r
+                        float v;
+                        if constexpr (R == 1) v = y[u];
+                        if constexpr (R == 2) v = fold32(y[u], y[u + 1]);
+                        if constexpr (R == 4) v = fold16(fold32(y[u], y[u + 2]), fold32(y[u + 1], y[u + 3]));
+                        sY[buf][wave][u0 + u + (int)lane / CHW][lane % CHW] = v;
+                    }
+                }
+            }
+            __syncthreads();
+        }
+        if (!have) return;
+        if constexpr (OUT) {
+            if (last && p.h_out) store_state<S>(p.h_out + (size_t)b * slice + own, h);
+        } else {
+            store_state<S>(seg_h + seg * slice + own, h);
+            if (n0 == 0) p.seg_dt[((size_t)b * p.seg_count + seg) * p.C + c] = sum;
+        }
+        return;
     }
 
-    // the thread's part of a tile
-    const int row = (int)tid / PER_ROW, col = (int)(tid % PER_ROW) * CH, ch0 = c0 + col;
+    if (!OUT && last) return;
+    const int tid = (int)threadIdx.x - 64 * kScanWaves;
+    const int row = tid / PER_ROW, col = tid % PER_ROW * CH, ch0 = c0 + col;
     const int live = min(max(p.C - ch0, 0), CH);                                  // channels that there are
+    const int brow = tid * BC / (2 * N), bcol = tid * BC % (2 * N);               // the token of B and C, and where in that token's 2N values
+    const bool is_c = bcol >= N;
     float bias[CH], D[CH];
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         const int at = min(ch0 + i, p.C - 1);
         bias[i] = p.dt_bias ? p.dt_bias[at] : 0.f;
-        D[i] = p.D[at];
+        D[i] = OUT ? p.D[at] : 0.f;
     }
-    const size_t tok0 = (size_t)b * p.L;
-    Piece<IO, CH> x, dt, z, nx, ndt, nz;
-    auto fetch = [&](int t0, Piece<IO, CH> &px, Piece<IO, CH> &pdt, Piece<IO, CH> &pz) {
+    const void *bc = is_c ? p.Cm : p.Bm;
+    const size_t bc_stride = is_c ? p.c_stride : p.b_stride;
+    constexpr int ES = IO == SSMV_BF16 ? 2 : 4, BCW = BC * ES / 4;
+    Piece<IO, CH> nx, ndt, nz, px, pz, ex, ez;                                    // fetched; of the tile being scanned; of the one behind it
+    uint32_t nbc[BCW];
+    // where the thread's next pieces are: a tile further after every access
+    const size_t tok = tok0 + from + row;
+    const char *x_at = static_cast<const char *>(p.x) + (tok * p.x_stride + ch0) * ES, *dt_at = static_cast<const char *>(p.dt) + (tok * p.dt_stride + ch0) * ES;
+    const char *z_at = static_cast<const char *>(p.z) + (tok * p.z_stride + ch0) * ES, *bc_at = static_cast<const char *>(bc) + ((tok0 + from + brow) * bc_stride + bcol % N) * ES;
+    char *y_at = static_cast<char *>(p.y) + (tok * p.y_stride + ch0) * ES;
+    auto fetch = [&](int t0) {
         const int n = t0 + row < len ? live : 0;                                  // what lies behind a sequence's tokens is not read
-        const size_t tok = tok0 + t0 + row;
-        px.template load<VEC>(p.x, tok * p.x_stride + ch0, n);
-        pdt.template load<VEC>(p.dt, tok * p.dt_stride + ch0, n);
-        if (p.z) pz.template load<VEC>(p.z, tok * p.z_stride + ch0, n);
+        nx.template load<VEC>(x_at, 0, n);
+        ndt.template load<VEC>(dt_at, 0, n);
+        if (OUT && p.z) nz.template load<VEC>(z_at, 0, n);
+        const bool there = t0 + brow < len && (OUT || !is_c);
+#pragma unroll
+        for (int i = 0; i < BCW; ++i) nbc[i] = there ? reinterpret_cast<const uint32_t *>(bc_at)[i] : 0u;
+        x_at += T * ES * p.x_stride; dt_at += T * ES * p.dt_stride; z_at += T * ES * p.z_stride; bc_at += T * ES * bc_stride;
     };
-    if (len > 0) fetch(0, nx, ndt, nz);
-
-    for (int t0 = 0; t0 < len; t0 += T) {
-        const int n = min(len - t0, T);
-        x = nx; dt = ndt; z = nz;
-        {
-            float2 in[CH];
+    auto prepare = [&](int t0, int buf) {
+        float2 in[CH];
 #pragma unroll
-            for (int i = 0; i < CH; ++i) {
-                float d = dt.get(i);
-                if (p.softplus) d = softplus_series(d + bias[i]);
-                d = row < n ? d : 0.f;                                            // tokens that are none leave the state as it is
-                in[i] = make_float2(d, d * x.get(i));
-            }
-#pragma unroll
-            for (int i = 0; i < CH; i += 2) *reinterpret_cast<float4 *>(&sIn[row][col + i]) = make_float4(in[i].x, in[i].y, in[i + 1].x, in[i + 1].y);
+        for (int i = 0; i < CH; ++i) {
+            float d = ndt.get(i);
+            if (p.softplus) d = softplus_exact(d + bias[i]);
+            d = t0 + row < len ? d : 0.f;                                         // tokens that are none leave the state as it is
+            in[i] = make_float2(d, d * nx.get(i));
         }
-        __syncthreads();
-        if (t0 + T < len) fetch(t0 + T, nx, ndt, nz);
-        const int e = IO == SSMV_BF16 ? 2 : 4;
-        for (int u0 = 0; u0 < n; u0 += U) {
-            Coef<IO, S> B[U], C[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const size_t tok = tok0 + min(t0 + u0 + u, len - 1);
-                B[u].load(static_cast<const char *>(p.Bm) + (tok * p.b_stride + wave * S) * e);
-                C[u].load(static_cast<const char *>(p.Cm) + (tok * p.c_stride + wave * S) * e);
-            }
+        for (int i = 0; i < CH; i += 2) *reinterpret_cast<float4 *>(&sIn[buf][row][col + i]) = make_float4(in[i].x, in[i].y, in[i + 1].x, in[i + 1].y);
+        if (OUT || !is_c) {
+            float *to = is_c ? &sC[buf][OUT ? brow : 0][bcol % N] : &sB[buf][brow][bcol];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const float2 in = sIn[u0 + u][lane];
-                float y = 0.f;
-#pragma unroll
-                for (int i = 0; i < S; ++i) {
-                    h[i] = fmaf(h[i], __builtin_amdgcn_exp2f(a[i] * in.x), in.y * B[u].get(i));
-                    y = fmaf(h[i], C[u].get(i), y);
-                }
-                sY[wave][u0 + u][lane] = y;
+            for (int i = 0; i < BC; i += 2) {
+                float2 v;
+                if constexpr (IO == SSMV_BF16) v = make_float2(__uint_as_float(nbc[i / 2] << 16), __uint_as_float(nbc[i / 2] & 0xffff0000u));
+                else v = make_float2(__uint_as_float(nbc[i]), __uint_as_float(nbc[i + 1]));
+                *reinterpret_cast<float2 *>(to + i) = v;
             }
         }
-        __syncthreads();
-        if (row < n) {
-            float y[CH];
+    };
+    auto finish = [&](int t0, int buf) {
+        if (!OUT || t0 + row >= len) return;
+        float y[CH];
+        char *to = y_at;
+        y_at += T * ES * p.y_stride;
 #pragma unroll
-            for (int i = 0; i < CH; ++i) y[i] = D[i] * x.get(i);
+        for (int i = 0; i < CH; ++i) y[i] = D[i] * ex.get(i);
 #pragma unroll
-            for (int w = 0; w < NW; ++w)
+        for (int w = 0; w < kScanWaves; ++w) {
+            const v4 t = *reinterpret_cast<const v4 *>(&sY[buf][w][OUT ? row : 0][col]);
 #pragma unroll
-                for (int i = 0; i < CH; ++i) y[i] += sY[w][row][col + i];
-            if (p.z)
-#pragma unroll
-                for (int i = 0; i < CH; ++i) y[i] *= silu_fast(z.get(i));
-            store_piece<IO, CH, VEC>(p.y, (tok0 + t0 + row) * p.y_stride + ch0, y, live);
+            for (int i = 0; i < CH; ++i) y[i] += t[i];
         }
+        if (p.z)
+#pragma unroll
+            for (int i = 0; i < CH; ++i) y[i] *= silu_fast(ez.get(i));
+        store_piece<IO, CH, VEC>(to, 0, y, live);
+    };
+    if (from < len) {
+        fetch(from);
+        prepare(from, 0);
+        px = nx; pz = nz;
+        if (from + T < len) fetch(from + T);
     }
-    if (p.h_out && have)
-#pragma unroll
-        for (int i = 0; i < S; i += 4) *reinterpret_cast<v4 *>(p.h_out + (size_t)b * p.C * N + own + i) = v4{h[i], h[i + 1], h[i + 2], h[i + 3]};
+    __syncthreads();
+    int buf = 0, t0 = from;
+    for (; t0 < len; t0 += T, buf ^= 1) {                                         // beside the scan of the tile at t0
+        if (t0 > from) finish(t0 - T, buf ^ 1);
+        ex = px; ez = pz;
+        if (t0 + T < len) {
+            prepare(t0 + T, buf ^ 1);
+            px = nx; pz = nz;
+            if (t0 + 2 * T < len) fetch(t0 + 2 * T);
+        }
+        __syncthreads();
+    }
+    if (t0 > from) finish(t0 - T, buf ^ 1);
 }
 
-template <int IO, int N, int S>
+template <int IO, int N, int CHW>
 int launch(const ScanParams &p, hipStream_t stream)
 {
-    const dim3 grid((unsigned)((p.C + kChannels - 1) / kChannels), (unsigned)p.batch), block(64 * (N / S));
-    if (p.vec) hipLaunchKernelGGL((selective_scan_kernel<IO, N, S, true>), grid, block, 0, stream, p);
-    else hipLaunchKernelGGL((selective_scan_kernel<IO, N, S, false>), grid, block, 0, stream, p);
+    const unsigned blocks = (unsigned)((p.C + CHW - 1) / CHW);
+    const dim3 block(64 * (kScanWaves + kHelpWaves)), ends(blocks, p.seg_count - 1, p.batch), all(blocks, p.seg_count, p.batch);
+    if (p.seg_count > 1) {
+        if (p.vec) hipLaunchKernelGGL((selective_scan_kernel<IO, N, CHW, true, false>), ends, block, 0, stream, p);
+        else hipLaunchKernelGGL((selective_scan_kernel<IO, N, CHW, false, false>), ends, block, 0, stream, p);
+        const int e = (int)hipGetLastError();
+        if (e != 0) return e;
+    }
+    if (p.vec) hipLaunchKernelGGL((selective_scan_kernel<IO, N, CHW, true, true>), all, block, 0, stream, p);
+    else hipLaunchKernelGGL((selective_scan_kernel<IO, N, CHW, false, true>), all, block, 0, stream, p);
     return (int)hipGetLastError();
+}
+
+template <int IO, int N>
+int launch_width(const ScanParams &p, hipStream_t stream)
+{
+    if constexpr (N < 64) if (p.channels_wg == 16) return launch<IO, N, 16>(p, stream);
+    return p.channels_wg == 32 ? launch<IO, N, 32>(p, stream) : launch<IO, N, 64>(p, stream);
 }
 
 template <int IO>
 int launch_n(const ScanParams &p, hipStream_t stream)
 {
     switch (p.N) {
-        case 16: return launch<IO, 16, 4>(p, stream);
-        case 32: return launch<IO, 32, 8>(p, stream);
-        case 64: return launch<IO, 64, 8>(p, stream);
+        case 16: return launch_width<IO, 16>(p, stream);
+        case 32: return launch_width<IO, 32>(p, stream);
+        case 64: return launch_width<IO, 64>(p, stream);
     }
     return (int)hipErrorInvalidValue;
 }

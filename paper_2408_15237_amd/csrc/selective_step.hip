@@ -43,7 +43,7 @@ __global__ __launch_bounds__(256) void selective_step_kernel(const TokenParams p
     const float D = p.D[hd], bias = p.dt_bias ? p.dt_bias[hd] : 0.f;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const float d = p.softplus ? softplus_fast(dt[u] + bias) : dt[u];
+        const float d = p.softplus ? softplus_exact(dt[u] + bias) : dt[u];
         const float dx = d * x[u];
         float y = 0.f;
         if constexpr (DIAG) {
