@@ -818,22 +818,23 @@ static int check_beam_sizes(int batch, int beams_in, int beams_out, int vocab)
 }
 
 // keys [row][piece][keep], then sums [row][piece]
-static size_t beam_layout(int batch, int beams_in, int beams_out, int vocab, int *pieces, int *keep, size_t *sums_at)
+static size_t beam_layout(int batch, int beams_in, int beams_out, int vocab, BeamPlan *plan, int *keep, size_t *sums_at)
 {
     const int rows = batch * beams_in;
-    *pieces = beam_pieces(rows, vocab);
     *keep = beams_out < vocab ? beams_out : vocab;
-    *sums_at = ((size_t)rows * *pieces * *keep * sizeof(unsigned long long) + 15) / 16 * 16;
-    return *sums_at + ((size_t)rows * *pieces * sizeof(float2) + 15) / 16 * 16;
+    *plan = beam_plan(rows, vocab, *keep);
+    *sums_at = ((size_t)rows * plan->pieces * *keep * sizeof(unsigned long long) + 15) / 16 * 16;
+    return *sums_at + ((size_t)rows * plan->pieces * sizeof(float2) + 15) / 16 * 16;
 }
 
 int ssmv_beam_workspace(int32_t batch, int32_t beams_in, int32_t beams_out, int32_t vocab, size_t *out_bytes)
 {
     TRY(check_beam_sizes(batch, beams_in, beams_out, vocab));
     if (!out_bytes) return fail(SSMV_EINVAL, "out_bytes is NULL");
-    int pieces, keep;
+    BeamPlan plan;
+    int keep;
     size_t at;
-    *out_bytes = beam_layout(batch, beams_in, beams_out, vocab, &pieces, &keep, &at);
+    *out_bytes = beam_layout(batch, beams_in, beams_out, vocab, &plan, &keep, &at);
     return SSMV_OK;
 }
 
@@ -859,9 +860,10 @@ int ssmv_beam_select(const ssmv_beam_args *args, void *hip_stream)
     p.logits = a.logits; p.scores = a.scores; p.done = a.done; p.parent = a.parent; p.token = a.token; p.scores_out = a.scores_out; p.done_out = a.done_out;
     p.row_stride = a.row_stride;
     p.batch = a.batch; p.beams_in = a.beams_in; p.beams_out = a.beams_out; p.V = a.vocab; p.io = a.io_dtype; p.eos = a.eos;
-    p.vec = wide(a.logits, a.row_stride, p.io);
+    BeamPlan plan;
     size_t sums_at;
-    beam_layout(a.batch, a.beams_in, a.beams_out, a.vocab, &p.pieces, &p.keep, &sums_at);
+    beam_layout(a.batch, a.beams_in, a.beams_out, a.vocab, &plan, &p.keep, &sums_at);
+    p.small = plan.small; p.pieces = plan.pieces; p.piece_len = plan.len; p.chunks = plan.chunks;
     p.keys = static_cast<unsigned long long *>(a.workspace);
     p.sums = reinterpret_cast<float2 *>(static_cast<char *>(a.workspace) + sums_at);
     const int hc = launch_beam_select(p, (hipStream_t)hip_stream);

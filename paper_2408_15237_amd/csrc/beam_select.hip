@@ -5,6 +5,7 @@ namespace ssmv {
 namespace {
 
 typedef unsigned long long Key;
+constexpr float kTop = 3.402823466e+38f;                                        // the largest finite value
 
 // A candidate of a row as a whole number: larger is better - the logit in an order-preserving form above, the token's
 // complement below, so that keys are unique and equal logits go by the lower token.  0 stands for none.
@@ -21,182 +22,301 @@ __device__ __forceinline__ float key_logit(Key k)
 }
 __device__ __forceinline__ unsigned key_token(Key k) { return 0xffffffffu - (unsigned)k; }
 
-// NaN is a token that is not allowed, +inf the largest finite logit
-__device__ __forceinline__ float clean(float v) { return v != v ? -INFINITY : fminf(v, 3.402823466e+38f); }
+constexpr int THREADS = 256, WAVES = THREADS / 64;
+constexpr int kList = 1024;                                                       // candidates that the short way of a piece may collect
 
-constexpr int THREADS = 256, E = kBeamPiece / THREADS;
-
-// The best `keep` candidates of a piece of a row, best first, and its part of the row's sum.
-// The keep-th largest of the threads' best keys is a bound that at least `keep` candidates reach, and only the keep threads at or above
-// it can hold any: what reaches it is collected (at most keep * E keys, usually little more than keep) and ranked.
-template <int IO, bool VEC>
+// The best `keep` candidates of a piece of a row, best first, and its part of the row's sum; E logits of a thread at a time.
+// The threads form at least `keep` groups of equal size; the least of the groups' largest logits is a bound that at least `keep`
+// logits reach, and what reaches it is collected and ranked - some tens of candidates.  Where ties make them too many, the
+// bound is taken of the threads' best keys, which are unique: only the `keep` threads at or above it can hold any candidate, keep * E at most.
+// A row may begin anywhere: its vectors are read where its own elements lie (16 bytes at the alignment of an element), so that which
+// thread takes a token, and with it the order of the sum, does not depend on the address, and equal rows stay equal to the last bit.
+template <int IO, int E>
 __global__ __launch_bounds__(THREADS) void beam_piece_kernel(const BeamParams p)
 {
-    __shared__ Key sBest[THREADS];
-    __shared__ Key sList[SSMV_BEAMS_MAX * E];
-    __shared__ float sMax[THREADS / 64], sSum[THREADS / 64];
-    __shared__ Key sBound;
+    constexpr int EV = IoVec<IO>::EV, CHUNK = THREADS * E, ES = IO == SSMV_BF16 ? 2 : 4;
+    constexpr int kMost = (E > 8 ? SSMV_BEAMS_MAX : kSmallKeep) * E;              // of the long way; the list has room for both
+    constexpr float LOG2E = 1.4426950408889634f;
+    __shared__ Key sList[kList + kMost];
+    __shared__ Key sBest[SSMV_BEAMS_MAX], sThread[THREADS];
+    __shared__ __attribute__((aligned(16))) float sMax[SSMV_BEAMS_MAX];
+    __shared__ float sSum[WAVES];
+    __shared__ Key sKey;
     __shared__ int sCount;
     const unsigned tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
-    const unsigned piece = blockIdx.x;
+    const int piece = blockIdx.x, keep = p.keep;
     const size_t row = blockIdx.y;
     if (p.done && p.done[row] != 0) return;                                       // a finished row's logits are not read
-    const unsigned first = piece * kBeamPiece, n = min((unsigned)p.V - first, (unsigned)kBeamPiece);
-    constexpr int EV = VEC ? IoVec<IO>::EV : 1;
-    float v[E];
-    const size_t at = row * p.row_stride + first;
-    auto token = [&](int i) { return (unsigned)(i / EV) * (THREADS * EV) + tid * EV + i % EV; };       // of the piece
+    const char *base = static_cast<const char *>(p.logits) + row * p.row_stride * ES;
+    Key *out = p.keys + (row * p.pieces + piece) * keep;
+    const int size = keep <= 4 ? 64 : keep <= 8 ? 32 : keep <= 16 ? 16 : keep <= 32 ? 8 : 4, groups = THREADS / size;
+
+    const int begin = piece * p.piece_len, end = min(p.V, begin + p.piece_len);
+    float m = -kTop, sum = 0.f, bound = -INFINITY;                                // of the chunks so far
+    // A thread's vectors of a chunk, all requested before the first is used, and a chunk ahead of its arithmetic.  One that reaches past the
+    // end is moved back to it: the tokens ahead of its own place, which are another vector's, hold -inf then.
+    uint4 raw[E / EV];
+    auto fetch = [&](int first) {
 #pragma unroll
-    for (int i = 0; i < E; i += EV) {
-        const unsigned t = token(i);
-        if constexpr (VEC) {
-            float d[EV];
-            if (t + EV <= n) {
-                IoVec<IO>::load(p.logits, at + t, d);
+        for (int i = 0; i < E / EV; ++i) {
+            const int at = min(first + i * (THREADS * EV) + (int)tid * EV, end - EV);
+            __builtin_memcpy(&raw[i], base + (ptrdiff_t)at * ES, sizeof(uint4));
+        }
+    };
+    if (end >= EV) fetch(begin);
+    if (tid == 0) sCount = 0;
+    // the places of the list's first `count` keys: a quad of lanes to a key
+    auto rank = [&](int count, Key *to) {
+        for (int i = tid / 4; i < count; i += THREADS / 4) {
+            const Key k = sList[i];
+            int r = 0;
+#pragma unroll 4
+            for (int j = tid % 4; j < count; j += 4) r += sList[j] > k;
+            r += __shfl_xor(r, 1);
+            r += __shfl_xor(r, 2);
+            if (r < keep && tid % 4 == 0) to[r] = k;
+        }
+    };
+    for (int chunk = 0; chunk < p.chunks; ++chunk) {
+        const int first = begin + chunk * CHUNK;
+        auto place = [&](int i) { return first + (i / EV) * (THREADS * EV) + (int)tid * EV; };
+        auto pos = [&](int i) { return min(place(i), end - EV) + i % EV; };
+        auto there = [&](int i) { return pos(i) >= place(i); };
+        float v[E];
+        if (end >= EV) {
 #pragma unroll
-                for (int j = 0; j < EV; ++j) v[i + j] = clean(d[j]);
-            } else {
+            for (int i = 0; i < E / EV; ++i) {
+                float d[EV];
+                IoVec<IO>::decode(raw[i], d);
 #pragma unroll
-                for (int j = 0; j < EV; ++j) v[i + j] = t + j < n ? clean(load_io(p.logits, at + t + j, IO)) : -INFINITY;
+                for (int j = 0; j < EV; ++j) v[i * EV + j] = d[j];
             }
-        } else {
-            v[i] = t < n ? clean(load_io(p.logits, at + t, IO)) : -INFINITY;
+            if (first + CHUNK > end) {
+#pragma unroll
+                for (int i = 0; i < E; ++i) v[i] = there(i) ? v[i] : -INFINITY;
+            }
+            if (chunk + 1 < p.chunks) fetch(first + CHUNK);
+        } else {                                                                  // a vocabulary of less than one vector
+#pragma unroll
+            for (int i = 0; i < E; ++i) v[i] = i < EV && there(i) && pos(i) >= 0 ? load_io(base, (size_t)pos(i), IO) : -INFINITY;
+        }
+        float most = -INFINITY;                                                   // (the maximum of a number and NaN is the number)
+#pragma unroll
+        for (int i = 0; i < E; ++i) most = fmaxf(most, v[i]);
+        float group = most;
+        for (int o = 1; o < size; o *= 2) group = fmaxf(group, __shfl_xor(group, o));
+        if (tid % size == 0) sMax[tid / size] = group;
+        __syncthreads();
+        const float before = m;
+        float least = INFINITY;
+        for (int g = 0; g < groups; g += 4) {
+            const float4 t = *reinterpret_cast<const float4 *>(sMax + g);
+            m = fmaxf(fmaxf(fmaxf(m, t.x), fmaxf(t.y, t.z)), t.w);
+            least = fminf(fminf(least, t.x), fminf(fminf(t.y, t.z), t.w));
+        }
+        if (m == INFINITY) {                                                      // +inf is the largest finite logit
+            m = kTop;
+            least = fminf(least, kTop);
+            most = fminf(most, kTop);
+#pragma unroll
+            for (int i = 0; i < E; ++i) v[i] = v[i] == INFINITY ? kTop : v[i];
+        }
+        bound = fmaxf(bound, least);
+        const int held = sCount;                                                  // candidates of the chunks before
+        const bool open = bound == -INFINITY;                                     // a group without a token that is allowed
+        __syncthreads();
+        unsigned hits = 0;
+        int at = 0, near = 0;
+        float logit = 0.f;
+        auto token = [&](unsigned bits) {                                         // of the lowest set bit
+            const int i = E - 1 - __builtin_ctz(bits);
+            return min(first + i / EV * (THREADS * EV) + (int)tid * EV, end - EV) + i % EV;
+        };
+        if (!open && most >= bound) {
+#pragma unroll
+            for (int i = 0; i < E; ++i) hits = 2 * hits + (v[i] >= bound);
+            at = atomicAdd(&sCount, __builtin_popcount(hits));
+            near = token(hits);
+            logit = load_io(base, (size_t)near, IO);                              // once more, out of the cache; back by when the sum is done
+        }
+        // exp(v - m) as one fused operation and exp2: the reference is what m log2 e rounds to, and the sum is corrected for that
+        const bool far = fabsf(m) > 1e30f;                                        // (where the products would overflow: the difference first)
+        const float ref = far ? 0.f : m * LOG2E;
+        auto total = [&]() {
+            float t = 0.f;
+            if (far) {
+#pragma unroll
+                for (int i = 0; i < E; ++i) t += __builtin_amdgcn_exp2f((v[i] - m) * LOG2E);
+                return t;
+            }
+#pragma unroll
+            for (int i = 0; i < E; ++i) t += __builtin_amdgcn_exp2f(fmaf(v[i], LOG2E, -ref));
+            return t * __builtin_amdgcn_exp2f(-fmaf(m, LOG2E, -ref));
+        };
+        float part = total();
+        if (part != part) {                                                       // NaN is a token that is not allowed
+#pragma unroll
+            for (int i = 0; i < E; ++i) v[i] = v[i] != v[i] ? -INFINITY : v[i];
+            part = total();
+        }
+        sum = fmaf(sum, __builtin_amdgcn_exp2f((before - m) * LOG2E), part);
+        while (hits && at < kList) {                                              // one, hardly ever more
+            sList[at++] = key_of(logit == INFINITY ? kTop : logit, (unsigned)near);
+            hits &= hits - 1;
+            if (hits) {
+                near = token(hits);
+                logit = load_io(base, (size_t)near, IO);
+            }
+        }
+        const bool final = chunk + 1 == p.chunks;
+        if (final) {
+            float all = sum;
+#pragma unroll
+            for (int o = 32; o > 0; o /= 2) all += __shfl_xor(all, o);
+            if (lane == 0) sSum[wave] = all;
+        }
+        __syncthreads();
+        int count = sCount;
+        if (open || count > kList) {                                              // the same for all threads
+            Key best = 0;
+#pragma unroll
+            for (int i = 0; i < E; ++i)
+                if (there(i)) {
+                    const Key k = key_of(v[i], (unsigned)pos(i));
+                    best = k > best ? k : best;
+                }
+            sThread[tid] = best;
+            if (tid == 0) sKey = 1;                                               // every candidate there is
+            __syncthreads();
+            int r = 0;
+#pragma unroll 8
+            for (int i = 0; i < THREADS; ++i) r += sThread[i] > best;
+            if (best != 0 && r == keep - 1) sKey = best;                          // keys are unique: one thread
+            if (tid == 0) sCount = held;
+            __syncthreads();
+            const Key from = sKey;
+            if (best >= from)
+#pragma unroll
+                for (int i = 0; i < E; ++i)
+                    if (there(i)) {
+                        const Key k = key_of(v[i], (unsigned)pos(i));
+                        if (k >= from) sList[atomicAdd(&sCount, 1)] = k;          // held + keep * E at most
+                    }
+            __syncthreads();
+            count = sCount;
+        }
+        if (final) {
+            rank(count, out);
+            for (int i = count + (int)tid; i < keep; i += THREADS) out[i] = 0;
+            if (tid == THREADS - 1) {
+                float s = 0.f;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) s += sSum[w];
+                p.sums[row * p.pieces + piece] = make_float2(m, s);
+            }
+        } else if (count > kList / 4) {                                           // room for the next chunk's: the best alone
+            rank(count, sBest);
+            __syncthreads();
+            const int kept = min(count, keep);
+            if (tid < (unsigned)kept) sList[tid] = sBest[tid];
+            if (tid == 0) sCount = kept;
+            bound = fmaxf(bound, kept == keep ? key_logit(sBest[keep - 1]) : -INFINITY);
         }
     }
-    // ---- the piece's largest logit and sum
-    float m = -3.402823466e+38f;
-#pragma unroll
-    for (int i = 0; i < E; ++i) m = fmaxf(m, v[i]);
-#pragma unroll
-    for (int o = 32; o > 0; o /= 2) m = fmaxf(m, __shfl_xor(m, o));
-    if (lane == 0) sMax[wave] = m;
-    Key best = 0;
-#pragma unroll
-    for (int i = 0; i < E; ++i)
-        if (token(i) < n) {
-            const Key k = key_of(v[i], first + token(i));
-            best = k > best ? k : best;
-        }
-    sBest[tid] = best;
-    if (tid == 0) { sCount = 0; sBound = 1; }                                     // 1: every candidate there is
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) m = fmaxf(m, sMax[w]);
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < E; ++i) sum += __builtin_amdgcn_exp2f((v[i] - m) * 1.4426950408889634f);
-#pragma unroll
-    for (int o = 32; o > 0; o /= 2) sum += __shfl_xor(sum, o);
-    if (lane == 0) sSum[wave] = sum;
-    int rank = 0;
-    for (int i = 0; i < THREADS; ++i) rank += sBest[i] > best;
-    if (best != 0 && rank == p.keep - 1) sBound = best;                           // keys are unique: one thread at most
-    __syncthreads();
-    if (tid == 0) {
-        float s = 0.f;
-#pragma unroll
-        for (int w = 0; w < THREADS / 64; ++w) s += sSum[w];
-        p.sums[row * p.pieces + piece] = make_float2(m, s);
-    }
-    const Key bound = sBound;
-    if (best >= bound) {
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-            if (token(i) >= n) continue;
-            const Key k = key_of(v[i], first + token(i));
-            if (k >= bound) sList[atomicAdd(&sCount, 1)] = k;
-        }
-    }
-    __syncthreads();
-    const int count = sCount;
-    Key *out = p.keys + (row * p.pieces + piece) * p.keep;
-    for (int i = tid; i < count; i += THREADS) {
-        const Key k = sList[i];
-        int r = 0;
-        for (int j = 0; j < count; ++j) r += sList[j] > k;
-        if (r < p.keep) out[r] = k;
-    }
-    for (int i = count + tid; i < p.keep; i += THREADS) out[i] = 0;
 }
 
-// how many of a list's n keys, best first, are larger
-__device__ __forceinline__ int larger(const Key *list, int n, Key k)
+// A workgroup per sequence.  A wave per row merges the pieces: the largest of the lists' last keys is a bound that `keep` candidates reach,
+// what reaches it is moved together, and its places are counted.  Then the rows of the sequence in the same way, by their scores: equal
+// ones by their places, which are in the order of row and rank.
+__global__ __launch_bounds__(1024) void beam_merge_kernel(const BeamParams p)
 {
-    int lo = 0;
-    while (n > 0) {
-        const int half = n / 2;
-        if (list[lo + half] > k) { lo += half + 1; n -= half + 1; }
-        else n = half;
-    }
-    return lo;
-}
-
-// A workgroup per sequence: the pieces of each row merged, then the rows.  A candidate's place is its place in its own list plus the
-// number of better ones in each other list (they are sorted).
-__global__ __launch_bounds__(THREADS) void beam_merge_kernel(const BeamParams p)
-{
-    __shared__ Key sKeys[SSMV_BEAMS_MAX * SSMV_BEAMS_MAX];
+    __shared__ Key sLists[kMergeKeys];
     __shared__ double sScore[SSMV_BEAMS_MAX * SSMV_BEAMS_MAX];
-    const unsigned tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
-    const int W = p.beams_in, keep = p.keep;
+    __shared__ int sToken[SSMV_BEAMS_MAX * SSMV_BEAMS_MAX], sDone[SSMV_BEAMS_MAX];
+    __shared__ int sCount;
+    const unsigned tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6, waves = blockDim.x >> 6;
+    const int W = p.beams_in, keep = p.keep, pieces = p.pieces, n = pieces * keep;
     const size_t row0 = (size_t)blockIdx.x * W;
-    for (int r = wave; r < W; r += THREADS / 64) {
+    Key *list = sLists + (size_t)wave * n;
+    if (tid == 0) sCount = 0;
+    for (int r = wave; r < W; r += waves) {
         const size_t row = row0 + r;
+        const Key *from = p.keys + row * n;
+        // all that the row needs of memory at once, also where it turns out to be finished
+        const float2 part = (int)lane < pieces ? p.sums[row * pieces + lane] : make_float2(-kTop, 0.f);      // at most 64 pieces
+        Key bound = (int)lane < pieces ? from[lane * keep + keep - 1] : 0;
+        const int done = p.done ? p.done[row] : 0;
         float given = p.scores[row];
-        given = given != given ? -INFINITY : fminf(given, 3.402823466e+38f);
-        if (p.done && p.done[row] != 0) {
+#pragma unroll 4
+        for (int i = lane; i < n; i += 64) list[i] = from[i];
+        given = given != given ? -INFINITY : fminf(given, kTop);
+        if (lane == 0) sDone[r] = done;
+        if (done != 0) {
             for (int i = lane; i < keep; i += 64) {
-                sKeys[r * keep + i] = key_of(0.f, (unsigned)p.eos);
+                sToken[r * keep + i] = p.eos;
                 sScore[r * keep + i] = i == 0 ? (double)given : -INFINITY;
             }
             continue;
         }
-        const float2 *sums = p.sums + row * p.pieces;
-        float m = -3.402823466e+38f;
-        for (int i = lane; i < p.pieces; i += 64) m = fmaxf(m, sums[i].x);
-        for (int o = 32; o > 0; o /= 2) m = fmaxf(m, __shfl_xor(m, o));
-        double s = 0.0;
-        for (int i = lane; i < p.pieces; i += 64) s += (double)sums[i].y * (double)__builtin_amdgcn_exp2f((sums[i].x - m) * 1.4426950408889634f);
-        for (int o = 32; o > 0; o /= 2) s += __shfl_xor(s, o);
-        const double lse = log(s);
-        const Key *lists = p.keys + row * p.pieces * keep;
-        for (int i = lane; i < p.pieces * keep; i += 64) {
-            const Key k = lists[i];
-            if (k == 0) continue;
-            const int own = i / keep;
-            int rank = i - own * keep;
-            for (int q = 0; q < p.pieces; ++q)
-                if (q != own) rank += larger(lists + q * keep, keep, k);
+        float m = part.x;
+        for (int o = 1; o < pieces; o *= 2) {
+            m = fmaxf(m, __shfl_xor(m, o));
+            const Key other = __shfl_xor(bound, o);
+            bound = other > bound ? other : bound;
+        }
+        m = __shfl(m, 0);
+        bound = __shfl(bound, 0);
+        double s = (double)part.y * (double)__builtin_amdgcn_exp2f((part.x - m) * 1.4426950408889634f);
+        for (int o = 1; o < pieces; o *= 2) s += __shfl_xor(s, o);
+        const double lse = log(__shfl(s, 0));
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");                    // the list is this wave's own
+        int count = 0;
+        for (int i0 = 0; i0 < n; i0 += 64) {                                      // a candidate moves down, never past one not looked at
+            const Key k = i0 + (int)lane < n ? list[i0 + lane] : 0;
+            const bool in = k != 0 && k >= bound;
+            const unsigned long long mask = __ballot(in);
+            if (in) list[count + __builtin_popcountll(mask & ((1ull << lane) - 1))] = k;
+            count += __builtin_popcountll(mask);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        for (int i = lane; i < count; i += 64) {
+            const Key k = list[i];
+            int rank = 0;
+#pragma unroll 8
+            for (int j = 0; j < count; ++j) rank += list[j] > k;
             if (rank < keep) {
                 const float l = key_logit(k);
-                sKeys[r * keep + rank] = k;
+                sToken[r * keep + rank] = (int)key_token(k);
                 sScore[r * keep + rank] = l == -INFINITY ? -INFINITY : (double)given + ((double)l - (double)m - lse);
             }
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");                    // before the next row's list
     }
     __syncthreads();
-    for (int i = tid; i < W * keep; i += THREADS) {
-        const int r = i / keep;
+    double bound = -INFINITY;
+    if (keep == p.beams_out)                                                      // a vocabulary of fewer tokens: all of them
+        for (int r = 0; r < W; ++r) bound = fmax(bound, sScore[r * keep + keep - 1]);
+    int *chosen = reinterpret_cast<int *>(sLists);                                // the lists are done with
+    for (int i = tid; i < W * keep; i += blockDim.x)
+        if (sScore[i] >= bound) chosen[atomicAdd(&sCount, 1)] = i;
+    __syncthreads();
+    const int count = sCount;
+    for (int c = tid; c < count; c += blockDim.x) {
+        const int i = chosen[c], r = i / keep;
         const double s = sScore[i];
-        int rank = i - r * keep;
-        for (int q = 0; q < W; ++q) {
-            if (q == r) continue;
-            int lo = 0, n = keep;                                                 // better: a larger score, or the same in a lower row
-            while (n > 0) {
-                const int half = n / 2;
-                const double o = sScore[q * keep + lo + half];
-                if (o > s || (o == s && q < r)) { lo += half + 1; n -= half + 1; }
-                else n = half;
-            }
-            rank += lo;
+        int rank = 0;
+#pragma unroll 4
+        for (int d = 0; d < count; ++d) {
+            const int j = chosen[d];
+            const double o = sScore[j];
+            rank += o > s || (o == s && j < i);
         }
         if (rank < p.beams_out) {
             const size_t at = (size_t)blockIdx.x * p.beams_out + rank, row = row0 + r;
-            const int token = (int)key_token(sKeys[i]);
             p.parent[at] = (int32_t)row;
-            p.token[at] = token;
+            p.token[at] = sToken[i];
             p.scores_out[at] = (float)s;
-            if (p.done_out) p.done_out[at] = (p.done && p.done[row] != 0) || token == p.eos;
+            if (p.done_out) p.done_out[at] = sDone[r] != 0 || sToken[i] == p.eos;
         }
     }
 }
@@ -205,19 +325,20 @@ __global__ __launch_bounds__(THREADS) void beam_merge_kernel(const BeamParams p)
 
 int launch_beam_select(const BeamParams &p, hipStream_t stream)
 {
-    const unsigned rows = (unsigned)p.batch * p.beams_in;
-    if (rows > 65535) return (int)hipErrorInvalidValue;                                    // refused by the host's checks
-    const dim3 grid((unsigned)p.pieces, rows);
+    const dim3 grid((unsigned)p.pieces, (unsigned)p.batch * p.beams_in);                    // at most 65535 rows (host)
     if (p.io == SSMV_BF16) {
-        if (p.vec) hipLaunchKernelGGL((beam_piece_kernel<SSMV_BF16, true>), grid, dim3(THREADS), 0, stream, p);
-        else hipLaunchKernelGGL((beam_piece_kernel<SSMV_BF16, false>), grid, dim3(THREADS), 0, stream, p);
+        if (p.small) hipLaunchKernelGGL((beam_piece_kernel<SSMV_BF16, 8>), grid, dim3(THREADS), 0, stream, p);
+        else hipLaunchKernelGGL((beam_piece_kernel<SSMV_BF16, 32>), grid, dim3(THREADS), 0, stream, p);
     } else {
-        if (p.vec) hipLaunchKernelGGL((beam_piece_kernel<SSMV_F32, true>), grid, dim3(THREADS), 0, stream, p);
-        else hipLaunchKernelGGL((beam_piece_kernel<SSMV_F32, false>), grid, dim3(THREADS), 0, stream, p);
+        if (p.small) hipLaunchKernelGGL((beam_piece_kernel<SSMV_F32, 8>), grid, dim3(THREADS), 0, stream, p);
+        else hipLaunchKernelGGL((beam_piece_kernel<SSMV_F32, 32>), grid, dim3(THREADS), 0, stream, p);
     }
     const int e = (int)hipGetLastError();
     if (e != 0) return e;
-    hipLaunchKernelGGL(beam_merge_kernel, dim3((unsigned)p.batch), dim3(THREADS), 0, stream, p);
+    int waves = kMergeKeys / (p.pieces * p.keep);                                           // at least 4 (beam_plan)
+    waves = waves < 16 ? waves : 16;
+    const int wanted = p.beams_in > 4 ? p.beams_in : 4;
+    hipLaunchKernelGGL(beam_merge_kernel, dim3((unsigned)p.batch), dim3(64 * (waves < wanted ? waves : wanted)), 0, stream, p);
     return (int)hipGetLastError();
 }
 

@@ -58,8 +58,7 @@ struct BeamParams {
     int32_t *done_out;
     size_t row_stride;
     int batch, beams_in, beams_out, V, io, eos;
-    int vec;                 // 1: 16-byte accesses of the logits
-    int pieces;              // parts of a row
+    int small, pieces, piece_len, chunks;   // see BeamPlan
     int keep;                // candidates kept of a row: min(beams_out, V)
     unsigned long long *keys;    // [row][piece][keep] the best of a part, best first; 0 = none
     float2 *sums;                // [row][piece] largest logit, sum of exp(logit - largest)
@@ -113,9 +112,28 @@ inline ScanPlan scan_plan(int batch, int C, int N, int L)
     return best;
 }
 
-constexpr int kBeamPiece = 8192;     // logits that a workgroup of the selection takes
+constexpr int kSmallKeep = 16;       // candidates of a small piece at most
+constexpr int kMergeKeys = 8192;     // keys that the merge of a sequence has room for: of four rows at least
 
-inline int beam_pieces(int rows, int V) { return (V + kBeamPiece - 1) / kBeamPiece; }
+struct BeamPlan {
+    int small;               // 1: chunks of 2048 logits, 0: of 8192
+    int pieces, len, chunks; // pieces of a row; logits of a piece (the last one's may be fewer); chunks of a piece
+};
+
+// Small chunks where large ones would be too few to fill the chip, and few candidates are kept of each.  Of large ones a piece takes
+// several where that leaves four workgroups for every compute unit.
+inline BeamPlan beam_plan(int rows, int V, int keep)
+{
+    BeamPlan r;
+    r.small = (long)rows * ((V + 8191) / 8192) < 512 && keep <= kSmallKeep && V <= 64 * 2048;
+    const int chunk = r.small ? 2048 : 8192, all = (V + chunk - 1) / chunk, align = r.small ? 8 : 64;
+    const int enough = (1024 + rows - 1) / rows, most = r.small ? 64 : enough < 32 ? enough : 32;
+    const int pieces = all < most ? all : most;
+    r.len = ((V + pieces - 1) / pieces + align - 1) / align * align;   // pieces alike: one that is nearly empty has no bound to offer
+    r.pieces = (V + r.len - 1) / r.len;
+    r.chunks = (r.len + chunk - 1) / chunk;
+    return r;
+}
 
 // Weak: a build of the argument checks alone (api.hip without the kernels) loads without them; its calls end on the host.
 __attribute__((weak)) int launch_causal_conv(const CausalConvParams &p, hipStream_t stream);
