@@ -367,8 +367,8 @@ int ssmv_stream_probe(int32_t mode, const void *src, void *dst0, void *dst1, siz
  *
  * Strides are in elements, between a sequence's tokens (or the rows of a single-token call); 0 = packed.  Sequences are L
  * strides apart, so that x and z, or B and C, may be parts of one projection's output.  Tensors of these calls need only the
- * alignment of their elements, but B and C rows 4 bytes; where all are 16-byte aligned, strides and channels too, accesses are
- * 16 bytes wide.  States (h_in, h_out), A and the workspaces: 16 bytes.  No output may overlap an input, but where it is said. */
+ * alignment of their elements, but B and C rows 4 bytes, and states (h_in, h_out), A [H][N] and the workspaces 16 bytes; what is
+ * aligned to 128 bytes is read fastest.  No output may overlap an input, but where it is said. */
 
 /* The causal depthwise convolution of conv1d_state_update over L tokens (L = 1: one new token of every row):
  *   out[b][t][c] = act(bias[c] + sum_{w<4} wgt[c][w] * raw_b[t-3+w][c]),  raw_b = the history of row src_row[b], then x[b],

@@ -641,8 +641,6 @@ int check_rows(int32_t *rows_in, int rows, const int32_t *src_row)
     return SSMV_OK;
 }
 
-bool wide(const void *p, int64_t stride, int io) { return aligned16(p) && stride % (io == SSMV_BF16 ? 8 : 4) == 0; }
-
 #define TRY(call) do { const int rc_ = (call); if (rc_ != SSMV_OK) return rc_; } while (0)
 
 }  // namespace
@@ -676,8 +674,6 @@ int ssm_causal_conv(const ssmv_conv_args *args, void *hip_stream)
     p.x = a.x; p.wgt = a.wgt; p.bias = a.bias; p.conv_in = a.conv_in; p.src_row = a.src_row; p.seq_len = a.seq_len; p.out = a.out; p.conv_out = a.conv_out;
     p.x_stride = a.x_stride; p.out_stride = a.out_stride;
     p.batch = a.batch; p.rows_in = a.rows_in; p.C = a.channels; p.L = a.L; p.io = a.io_dtype; p.act = a.act;
-    p.vec = wide(a.x, a.x_stride, p.io) && wide(a.out, a.out_stride, p.io) && wide(a.wgt, 0, p.io) && wide(a.bias, a.channels, p.io) &&
-            wide(a.conv_in, a.channels, p.io) && wide(a.conv_out, a.channels, p.io);
     const int hc = launch_causal_conv(p, (hipStream_t)hip_stream);
     return hc == 0 ? SSMV_OK : hip_fail(hc, "ssm_causal_conv");
 }
@@ -751,8 +747,6 @@ int ssm_selective_scan(const ssmv_scan_args *args, void *hip_stream)
     p.src_row = a.src_row; p.seq_len = a.seq_len; p.y = a.y_out; p.h_out = a.h_out;
     p.x_stride = a.x_stride; p.dt_stride = a.dt_stride; p.b_stride = a.b_stride; p.c_stride = a.c_stride; p.z_stride = a.z_stride; p.y_stride = a.y_stride;
     p.batch = a.batch; p.rows_in = a.rows_in; p.C = a.channels; p.N = a.dstate; p.L = a.L; p.io = a.io_dtype; p.softplus = a.dt_softplus;
-    p.vec = wide(a.x, a.x_stride, p.io) && wide(a.dt, a.dt_stride, p.io) && wide(a.z, a.z_stride, p.io) && wide(a.y_out, a.y_stride, p.io) &&
-            a.channels % 4 == 0;
     const int hc = launch_selective_scan(p, (hipStream_t)hip_stream);
     return hc == 0 ? SSMV_OK : hip_fail(hc, "ssm_selective_scan");
 }

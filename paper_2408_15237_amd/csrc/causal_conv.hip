@@ -7,20 +7,36 @@ namespace {
 
 constexpr int W = SSMV_CONV_WIDTH;
 
-// VEC elements of one token row: 16 bytes, or one element where the tensors do not allow more
+// VEC elements of one token row: 16 bytes, at the alignment of an element (aligned ones are as fast, others still much faster than an
+// element at a time), or one element where a row has fewer
 template <int IO, int VEC>
 struct Chunk {
     using Vec = IoVec<IO>;
+    static constexpr int ES = IO == SSMV_BF16 ? 2 : 4;
     static __device__ __forceinline__ uint4 zero() { return make_uint4(0, 0, 0, 0); }
     static __device__ __forceinline__ uint4 load(const void *base, size_t idx)
     {
-        if constexpr (VEC > 1) return Vec::load_raw(base, idx);
-        else return make_uint4(Vec::load_raw1(base, idx), 0, 0, 0);
+        if constexpr (VEC > 1) {
+            uint4 r;
+            __builtin_memcpy(&r, static_cast<const char *>(base) + idx * ES, sizeof(r));
+            return r;
+        } else {
+            return make_uint4(Vec::load_raw1(base, idx), 0, 0, 0);
+        }
     }
-    static __device__ __forceinline__ void store(void *base, size_t idx, uint4 r)
+    // its elements from `skip` on
+    static __device__ __forceinline__ void store(void *base, size_t idx, uint4 r, int skip)
     {
-        if constexpr (VEC > 1) Vec::store_raw(base, idx, r);
-        else Vec::store_raw1(base, idx, r.x);
+        if constexpr (VEC == 1) {
+            Vec::store_raw1(base, idx, r.x);
+        } else if (skip == 0) {
+            __builtin_memcpy(static_cast<char *>(base) + idx * ES, &r, sizeof(r));
+        } else {
+            const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+            for (int j = 1; j < VEC; ++j)
+                if (j >= skip) Vec::store_raw1(base, idx + j, IO == SSMV_BF16 ? w[j / 2] >> (j % 2 * 16) : w[j % 4]);
+        }
     }
     static __device__ __forceinline__ void decode(uint4 r, float (&v)[VEC])
     {
@@ -45,7 +61,9 @@ __global__ __launch_bounds__(256) void causal_conv_kernel(const CausalConvParams
     const unsigned lin = xcd_contiguous(blockIdx.y * gridDim.x + blockIdx.x, gridDim.x * gridDim.y);
     const unsigned b = lin / gridDim.x, item = (lin - b * gridDim.x) * 256 + threadIdx.x;
     if (item >= items) return;
-    const unsigned tile = item / chunks, c0 = (item - tile * chunks) * VEC;
+    // the last channels of a row: moved back to a whole vector, of which only what is the thread's own is stored
+    const unsigned tile = item / chunks, c_own = (item - tile * chunks) * VEC, c0 = min(c_own, (unsigned)p.C - VEC);
+    const int skip = (int)(c_own - c0);
     const int len = p.seq_len ? min(max(p.seq_len[b], 0), p.L) : p.L;
     const int t0 = (int)tile * T;
     const bool first = t0 == 0;
@@ -100,7 +118,7 @@ __global__ __launch_bounds__(256) void causal_conv_kernel(const CausalConvParams
                     for (int k = 0; k < W; ++k) o[j] = fmaf(w[j][k], v[(i + k) % W][j], o[j]);
                     if (p.act == SSMV_ACT_SILU) o[j] = silu_fast(o[j]);
                 }
-                Ch::store(p.out, (row0 + t0 + i) * p.out_stride + c0, Ch::encode(o));
+                Ch::store(p.out, (row0 + t0 + i) * p.out_stride + c0, Ch::encode(o), skip);
             }
         }
     }
@@ -111,7 +129,7 @@ __global__ __launch_bounds__(256) void causal_conv_kernel(const CausalConvParams
             uint4 r;
             if (t >= 0) r = x_at(t);
             else r = len == 0 ? hist[i] : len == 1 ? hist[i + 1 < W - 1 ? i + 1 : i] : hist[W - 2];       // len + i of the history
-            Ch::store(p.conv_out, ((size_t)b * (W - 1) + i) * p.C + c0, r);
+            Ch::store(p.conv_out, ((size_t)b * (W - 1) + i) * p.C + c0, r, skip);
         }
     }
 }
@@ -148,8 +166,8 @@ __global__ __launch_bounds__(256) void conv_history_kernel(const ConvHistoryPara
 int launch_causal_conv(const CausalConvParams &p, hipStream_t stream)
 {
     constexpr int EB = IoVec<SSMV_BF16>::EV, EF = IoVec<SSMV_F32>::EV;
-    if (p.io == SSMV_BF16) return p.vec && p.C % EB == 0 ? launch<SSMV_BF16, EB>(p, stream) : launch<SSMV_BF16, 1>(p, stream);
-    return p.vec && p.C % EF == 0 ? launch<SSMV_F32, EF>(p, stream) : launch<SSMV_F32, 1>(p, stream);
+    if (p.io == SSMV_BF16) return p.C >= EB ? launch<SSMV_BF16, EB>(p, stream) : launch<SSMV_BF16, 1>(p, stream);
+    return p.C >= EF ? launch<SSMV_F32, EF>(p, stream) : launch<SSMV_F32, 1>(p, stream);
 }
 
 int launch_conv_history(const ConvHistoryParams &p, hipStream_t stream)

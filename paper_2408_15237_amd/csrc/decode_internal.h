@@ -21,7 +21,6 @@ struct CausalConvParams {
     void *out, *conv_out;
     size_t x_stride, out_stride;
     int batch, rows_in, C, L, io, act;
-    int vec;                 // 1: 16-byte accesses everywhere
 };
 
 struct ScanParams {
@@ -32,7 +31,6 @@ struct ScanParams {
     float *h_out;
     size_t x_stride, dt_stride, b_stride, c_stride, z_stride, y_stride;
     int batch, rows_in, C, N, L, io, softplus;
-    int vec;                 // 1: 16-byte accesses of x, dt, z and y
     int channels_wg;         // channels of a workgroup: 64, 32, 16 (not with N = 64)
     int seg_len, seg_count;  // a cut prompt: tokens of a segment, segments of the longest prompt; seg_count 1: not cut
     float *seg_h;            // [batch][seg_count][C][N] end states of the segments, the first slice of each sequence; see selective_scan.hip

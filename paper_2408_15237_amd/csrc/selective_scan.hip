@@ -13,73 +13,46 @@ typedef float v4 __attribute__((ext_vector_type(4)));
 // CH values of adjacent channels as stored; behind the last channel zeros
 template <int IO, int CH>
 struct Piece {
-    static constexpr int NW = IO == SSMV_BF16 ? (CH + 1) / 2 : CH;
+    static constexpr int NW = IO == SSMV_BF16 ? CH / 2 : CH;
     uint32_t w[NW];
     __device__ __forceinline__ float get(int i) const
     {
         if constexpr (IO == SSMV_BF16) return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
         else return __uint_as_float(w[i]);
     }
-    template <bool VEC>
-    __device__ __forceinline__ void load(const void *base, size_t idx, int live)
+    // 8 or 16 bytes at the alignment of an element, but for the last channels of a row
+    __device__ __forceinline__ void load(const char *from, int live)
     {
-        if constexpr (VEC) {
-            const uint32_t *s = reinterpret_cast<const uint32_t *>(static_cast<const char *>(base) + idx * (IO == SSMV_BF16 ? 2 : 4));
-            if (live > 0) {
-                if constexpr (NW >= 4) {
-#pragma unroll
-                    for (int i = 0; i < NW; i += 4) {
-                        const uint4 t = *reinterpret_cast<const uint4 *>(s + i);
-                        w[i] = t.x; w[i + 1] = t.y; w[i + 2] = t.z; w[i + 3] = t.w;
-                    }
-                } else if constexpr (NW == 2) {
-                    const uint2 t = *reinterpret_cast<const uint2 *>(s);
-                    w[0] = t.x; w[1] = t.y;
-                } else {
-                    w[0] = *s;
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < NW; ++i) w[i] = 0;
-            }
+        if (live == CH) {
+            __builtin_memcpy(w, from, sizeof(w));
         } else {
             uint32_t v[CH];
 #pragma unroll
-            for (int i = 0; i < CH; ++i) v[i] = i < live ? IoVec<IO>::load_raw1(base, idx + i) : 0u;
+            for (int i = 0; i < CH; ++i) v[i] = i < live ? IoVec<IO>::load_raw1(from, i) : 0u;
 #pragma unroll
             for (int i = 0; i < NW; ++i) {
-                if constexpr (IO == SSMV_BF16) w[i] = v[2 * i] | (2 * i + 1 < CH ? v[2 * i + 1] << 16 : 0u);
+                if constexpr (IO == SSMV_BF16) w[i] = v[2 * i] | v[2 * i + 1] << 16;
                 else w[i] = v[i];
             }
         }
     }
 };
 
-template <int IO, int CH, bool VEC>
-__device__ __forceinline__ void store_piece(void *base, size_t idx, const float (&v)[CH], int live)
+template <int IO, int CH>
+__device__ __forceinline__ void store_piece(char *to, const float (&v)[CH], int live)
 {
-    if constexpr (VEC) {
-        if (live <= 0) return;
-        constexpr int NW = Piece<IO, CH>::NW;
-        uint32_t w[NW];
+    if (live == CH) {
+        uint32_t w[Piece<IO, CH>::NW];
 #pragma unroll
-        for (int i = 0; i < NW; ++i) {
+        for (int i = 0; i < Piece<IO, CH>::NW; ++i) {
             if constexpr (IO == SSMV_BF16) w[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
             else w[i] = __float_as_uint(v[i]);
         }
-        uint32_t *d = reinterpret_cast<uint32_t *>(static_cast<char *>(base) + idx * (IO == SSMV_BF16 ? 2 : 4));
-        if constexpr (NW >= 4) {
-#pragma unroll
-            for (int i = 0; i < NW; i += 4) *reinterpret_cast<uint4 *>(d + i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
-        } else if constexpr (NW == 2) {
-            *reinterpret_cast<uint2 *>(d) = make_uint2(w[0], w[1]);
-        } else {
-            d[0] = w[0];
-        }
+        __builtin_memcpy(to, w, sizeof(w));
     } else {
 #pragma unroll
         for (int i = 0; i < CH; ++i)
-            if (i < live) store_io(base, idx + i, v[i], IO);
+            if (i < live) store_io(to, i, v[i], IO);
     }
 }
 
@@ -142,7 +115,7 @@ constexpr int kScanWaves = 4, kHelpWaves = 4;
 // and stores, so that a tile's three stages run side by side and one barrier a tile is enough.  Everything changes hands in LDS.
 // B of a token is a broadcast operand: 16 / S tokens' worth sit in the lanes of every 16 of a register.
 // OUT false: only the state at the segment's end and the sum of its steps, of all segments but the last.
-template <int IO, int N, int CHW, bool VEC, bool OUT>
+template <int IO, int N, int CHW, bool OUT>
 __global__ __launch_bounds__(64 * (kScanWaves + kHelpWaves)) __attribute__((amdgpu_waves_per_eu(4)))
 void selective_scan_kernel(const ScanParams p)
 {
@@ -266,9 +239,9 @@ void selective_scan_kernel(const ScanParams p)
     char *y_at = static_cast<char *>(p.y) + (tok * p.y_stride + ch0) * ES;
     auto fetch = [&](int t0) {
         const int n = t0 + row < len ? live : 0;                                  // what lies behind a sequence's tokens is not read
-        nx.template load<VEC>(x_at, 0, n);
-        ndt.template load<VEC>(dt_at, 0, n);
-        if (OUT && p.z) nz.template load<VEC>(z_at, 0, n);
+        nx.load(x_at, n);
+        ndt.load(dt_at, n);
+        if (OUT && p.z) nz.load(z_at, n);
         const bool there = t0 + brow < len && (OUT || !is_c);
 #pragma unroll
         for (int i = 0; i < BCW; ++i) nbc[i] = there ? reinterpret_cast<const uint32_t *>(bc_at)[i] : 0u;
@@ -312,7 +285,7 @@ void selective_scan_kernel(const ScanParams p)
         if (p.z)
 #pragma unroll
             for (int i = 0; i < CH; ++i) y[i] *= silu_fast(ez.get(i));
-        store_piece<IO, CH, VEC>(to, 0, y, live);
+        store_piece<IO, CH>(to, y, live);
     };
     if (from < len) {
         fetch(from);
@@ -341,13 +314,11 @@ int launch(const ScanParams &p, hipStream_t stream)
     const unsigned blocks = (unsigned)((p.C + CHW - 1) / CHW);
     const dim3 block(64 * (kScanWaves + kHelpWaves)), ends(blocks, p.seg_count - 1, p.batch), all(blocks, p.seg_count, p.batch);
     if (p.seg_count > 1) {
-        if (p.vec) hipLaunchKernelGGL((selective_scan_kernel<IO, N, CHW, true, false>), ends, block, 0, stream, p);
-        else hipLaunchKernelGGL((selective_scan_kernel<IO, N, CHW, false, false>), ends, block, 0, stream, p);
+        hipLaunchKernelGGL((selective_scan_kernel<IO, N, CHW, false>), ends, block, 0, stream, p);
         const int e = (int)hipGetLastError();
         if (e != 0) return e;
     }
-    if (p.vec) hipLaunchKernelGGL((selective_scan_kernel<IO, N, CHW, true, true>), all, block, 0, stream, p);
-    else hipLaunchKernelGGL((selective_scan_kernel<IO, N, CHW, false, true>), all, block, 0, stream, p);
+    hipLaunchKernelGGL((selective_scan_kernel<IO, N, CHW, true>), all, block, 0, stream, p);
     return (int)hipGetLastError();
 }
 
