@@ -24,13 +24,18 @@ struct Chunk {
             return make_uint4(Vec::load_raw1(base, idx), 0, 0, 0);
         }
     }
-    // its elements from `skip` on
+    // its elements from `skip` on; PAST: past the caches
+    template <bool PAST>
     static __device__ __forceinline__ void store(void *base, size_t idx, uint4 r, int skip)
     {
         if constexpr (VEC == 1) {
             Vec::store_raw1(base, idx, r.x);
         } else if (skip == 0) {
-            __builtin_memcpy(static_cast<char *>(base) + idx * ES, &r, sizeof(r));
+            typedef uint32_t loose __attribute__((ext_vector_type(4), aligned(2)));
+            loose *to = reinterpret_cast<loose *>(static_cast<char *>(base) + idx * ES);
+            const loose v = {r.x, r.y, r.z, r.w};
+            if constexpr (PAST) __builtin_nontemporal_store(v, to);
+            else *to = v;
         } else {
             const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
@@ -52,22 +57,23 @@ struct Chunk {
 };
 
 // A thread owns VEC adjacent channels of T tokens: it requests its tokens and the three before them together, and slides over
-// them in registers.  The three are those of the thread of the tokens before, out of the L2; the first tokens take the history, and
-// their thread also leaves the newest three inputs, so that conv_out may be conv_in.
-template <int IO, int VEC, int T>
-__global__ __launch_bounds__(256) void causal_conv_kernel(const CausalConvParams p, unsigned chunks, unsigned items)
+// them in registers.  The three are those of the thread of the tokens before, 2^lanes threads ahead in the same workgroup but for one
+// tile in 256 / 2^lanes, so that they come out of the L1 and what a workgroup reads does not depend on where others run.  The first tokens
+// take the history, and their thread also leaves the newest three inputs, so that conv_out may be conv_in.
+template <int IO, int VEC, int T, bool PAST>
+__global__ __launch_bounds__(256) void causal_conv_kernel(const CausalConvParams p, int lanes, unsigned chunks, unsigned groups)
 {
     using Ch = Chunk<IO, VEC>;
-    const unsigned lin = xcd_contiguous(blockIdx.y * gridDim.x + blockIdx.x, gridDim.x * gridDim.y);
-    const unsigned b = lin / gridDim.x, item = (lin - b * gridDim.x) * 256 + threadIdx.x;
-    if (item >= items) return;
+    const unsigned b = blockIdx.y, run = blockIdx.x / groups, group = blockIdx.x - run * groups;       // groups of channels; runs of tiles
+    const unsigned chunk = (group << lanes) + (threadIdx.x & ((1u << lanes) - 1)), tile = (run << (8 - lanes)) + (threadIdx.x >> lanes);
+    if (chunk >= chunks) return;
     // the last channels of a row: moved back to a whole vector, of which only what is the thread's own is stored
-    const unsigned tile = item / chunks, c_own = (item - tile * chunks) * VEC, c0 = min(c_own, (unsigned)p.C - VEC);
+    const unsigned c_own = chunk * VEC, c0 = min(c_own, (unsigned)p.C - VEC);
     const int skip = (int)(c_own - c0);
     const int len = p.seq_len ? min(max(p.seq_len[b], 0), p.L) : p.L;
+    if (tile * (size_t)T >= (size_t)len && tile != 0) return;
     const int t0 = (int)tile * T;
     const bool first = t0 == 0;
-    if (t0 >= len && !first) return;
 
     const size_t row0 = (size_t)b * p.L;                       // the sequence's tokens
     auto x_at = [&](int t) { return Ch::load(p.x, (row0 + t) * p.x_stride + c0); };
@@ -118,7 +124,7 @@ __global__ __launch_bounds__(256) void causal_conv_kernel(const CausalConvParams
                     for (int k = 0; k < W; ++k) o[j] = fmaf(w[j][k], v[(i + k) % W][j], o[j]);
                     if (p.act == SSMV_ACT_SILU) o[j] = silu_fast(o[j]);
                 }
-                Ch::store(p.out, (row0 + t0 + i) * p.out_stride + c0, Ch::encode(o), skip);
+                Ch::template store<PAST>(p.out, (row0 + t0 + i) * p.out_stride + c0, Ch::encode(o), skip);
             }
         }
     }
@@ -129,7 +135,7 @@ __global__ __launch_bounds__(256) void causal_conv_kernel(const CausalConvParams
             uint4 r;
             if (t >= 0) r = x_at(t);
             else r = len == 0 ? hist[i] : len == 1 ? hist[i + 1 < W - 1 ? i + 1 : i] : hist[W - 2];       // len + i of the history
-            Ch::store(p.conv_out, ((size_t)b * (W - 1) + i) * p.C + c0, r, skip);
+            Ch::template store<false>(p.conv_out, ((size_t)b * (W - 1) + i) * p.C + c0, r, skip);
         }
     }
 }
@@ -139,14 +145,21 @@ int launch(const CausalConvParams &p, hipStream_t stream)
 {
     const unsigned chunks = (unsigned)((p.C + VEC - 1) / VEC);
     auto go = [&](auto kernel, int T) {
-        const size_t items = (size_t)((p.L + T - 1) / T) * chunks;
-        if (items > 0x7fffff00u || p.batch > 65535) return (int)hipErrorInvalidValue;      // refused by the host's checks
-        const dim3 grid((unsigned)((items + 255) / 256), (unsigned)p.batch);
-        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, p, chunks, (unsigned)items);
+        int lanes = 3;                                                            // up to 64 vectors of a row, the rest of the workgroup the tokens behind
+        while (lanes < 6 && (1u << lanes) < chunks) ++lanes;
+        if (T == 1 && chunks > 64) lanes = 8;                                     // one token: no others
+        const unsigned groups = (chunks + (1u << lanes) - 1) >> lanes, tiles = (unsigned)((p.L + T - 1) / T);
+        const size_t runs = ((size_t)tiles + (1u << (8 - lanes)) - 1) >> (8 - lanes);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(runs * groups), (unsigned)p.batch), dim3(256), 0, stream, p, lanes, chunks, groups);
         return (int)hipGetLastError();
     };
-    if (p.L == 1) return go(causal_conv_kernel<IO, VEC, 1>, 1);
-    return go(causal_conv_kernel<IO, VEC, 8>, 8);
+    if (p.L == 1) return go(causal_conv_kernel<IO, VEC, 1, false>, 1);
+    // Whatever comes next reads the outputs: they go through the caches as long as those can hold them (256 MB behind the L2s, which the
+    // inputs pass too).  Conv and a sum over its outputs, us, through / past the caches: 34 MB 56.0 / 63.7, 84 MB 122.8 / 129.1,
+    // 168 MB 277.7 / 270.4.
+    if constexpr (VEC > 1)
+        if ((size_t)p.batch * p.L * p.C * Chunk<IO, VEC>::ES > (128u << 20)) return go(causal_conv_kernel<IO, VEC, 8, true>, 8);
+    return go(causal_conv_kernel<IO, VEC, 8, false>, 8);
 }
 
 // a thread per element of conv_out
