@@ -100,6 +100,7 @@ class ssmv_cache(ctypes.Structure):
 
 
 _lib = None
+_byref = ctypes.byref
 
 
 def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
@@ -283,16 +284,16 @@ def ssmv_gated_rmsnorm(y, z, weight, rows: int, channels: int, group_size: int, 
 
 # ---- plain and beam decoding: from state to state -----------------------------------------------------------------------
 
-def _rows(t, rows_in, default: int) -> int:
-    """Rows of the state that goes in: as given, else the tensor's first dimension, else as many as go out."""
-    return rows_in if rows_in else t.shape[0] if hasattr(t, "shape") else default
+def _rows(t, rows_in, src_row) -> int:
+    """Rows of the state that goes in: as given, else the tensor's first dimension where an index looks at them, else 0 (as many as go out)."""
+    return rows_in or (0 if src_row is None or t is None or isinstance(t, int) else t.shape[0])
 
 
 def ssm_causal_conv(*, x, wgt, out, batch: int, channels: int, L: int, io, bias=None, act="none", conv_in=None, conv_out=None, src_row=None,
                     rows_in: int = 0, seq_len=None, x_stride: int = 0, out_stride: int = 0, stream=None) -> None:
     a = ssmv_conv_args(_ptr(x), _ptr(wgt), _ptr(bias), _ptr(conv_in), _ptr(src_row), _ptr(seq_len), _ptr(out), _ptr(conv_out), x_stride, out_stride,
-                       batch, _rows(conv_in, rows_in, batch), channels, L, IO_CODES.get(io, io), ACT_CODES.get(act, act))
-    _ck(load_library().ssm_causal_conv(ctypes.byref(a), _stream(stream)))
+                       batch, _rows(conv_in, rows_in, src_row), channels, L, IO_CODES.get(io, io), ACT_CODES.get(act, act))
+    _ck((_lib or load_library()).ssm_causal_conv(_byref(a), _stream(stream)))
 
 
 def ssm_selective_scan_workspace(batch: int, channels: int, dstate: int, L: int) -> int:
@@ -306,17 +307,17 @@ def ssm_selective_scan(*, x, dt, A, Bm, Cm, D, y_out, batch: int, channels: int,
                        b_stride: int = 0, c_stride: int = 0, z_stride: int = 0, y_stride: int = 0, workspace=None, stream=None) -> None:
     a = ssmv_scan_args(_ptr(x), _ptr(dt), _ptr(dt_bias), _ptr(A), _ptr(Bm), _ptr(Cm), _ptr(D), _ptr(z), _ptr(h_in), _ptr(src_row), _ptr(seq_len),
                        _ptr(y_out), _ptr(h_out), _ptr(workspace), x_stride, dt_stride, b_stride, c_stride, z_stride, y_stride,
-                       batch, _rows(h_in, rows_in, batch), channels, dstate, L, IO_CODES.get(io, io), dt_softplus)
-    _ck(load_library().ssm_selective_scan(ctypes.byref(a), _stream(stream)))
+                       batch, _rows(h_in, rows_in, src_row), channels, dstate, L, IO_CODES.get(io, io), dt_softplus)
+    _ck((_lib or load_library()).ssm_selective_scan(_byref(a), _stream(stream)))
 
 
 def ssm_selective_step(*, x, dt, A, Bm, Cm, D, y_out, h_in, h_out, rows: int, nheads: int, headdim: int, dstate: int, io, ngroups: int = 1,
                        a_mode="scalar", dt_bias=None, dt_softplus: bool = False, z=None, src_row=None, rows_in: int = 0, x_stride: int = 0,
                        dt_stride: int = 0, b_stride: int = 0, c_stride: int = 0, z_stride: int = 0, y_stride: int = 0, stream=None) -> None:
     a = ssmv_token_args(_ptr(x), _ptr(dt), _ptr(dt_bias), _ptr(A), _ptr(Bm), _ptr(Cm), _ptr(D), _ptr(z), _ptr(h_in), _ptr(src_row), _ptr(y_out),
-                        _ptr(h_out), x_stride, dt_stride, b_stride, c_stride, z_stride, y_stride, rows, _rows(h_in, rows_in, rows),
+                        _ptr(h_out), x_stride, dt_stride, b_stride, c_stride, z_stride, y_stride, rows, _rows(h_in, rows_in, src_row),
                         nheads, headdim, dstate, ngroups, IO_CODES.get(io, io), MODE_CODES.get(a_mode, a_mode), dt_softplus)
-    _ck(load_library().ssm_selective_step(ctypes.byref(a), _stream(stream)))
+    _ck((_lib or load_library()).ssm_selective_step(_byref(a), _stream(stream)))
 
 
 def ssmv_beam_workspace(batch: int, beams_in: int, beams_out: int, vocab: int) -> int:
@@ -329,7 +330,7 @@ def ssmv_beam_select(*, logits, scores, parent, token, scores_out, batch: int, b
                      row_stride: int = 0, done=None, done_out=None, eos: int = -1, stream=None) -> None:
     a = ssmv_beam_args(_ptr(logits), _ptr(scores), _ptr(done), _ptr(parent), _ptr(token), _ptr(scores_out), _ptr(done_out), _ptr(workspace), row_stride,
                        batch, beams_in, beams_out, vocab, IO_CODES.get(io, io), eos)
-    _ck(load_library().ssmv_beam_select(ctypes.byref(a), _stream(stream)))
+    _ck((_lib or load_library()).ssmv_beam_select(_byref(a), _stream(stream)))
 
 
 def ssmv_conv_history(dims, cache, conv_out, stream=None) -> None:

@@ -230,31 +230,35 @@ void selective_scan_kernel(const ScanParams p)
     const void *bc = is_c ? p.Cm : p.Bm;
     const size_t bc_stride = is_c ? p.c_stride : p.b_stride;
     constexpr int ES = IO == SSMV_BF16 ? 2 : 4, BCW = BC * ES / 4;
-    Piece<IO, CH> nx, ndt, nz, px, pz, ex, ez;                                    // fetched; of the tile being scanned; of the one behind it
-    uint32_t nbc[BCW];
+    struct Fetched {
+        Piece<IO, CH> x, dt, z;
+        uint32_t bc[BCW];
+    } even, odd;                                                                  // of the next tiles but one: two are on their way
+    Piece<IO, CH> px, pz, ex, ez;                                                 // of the tile being scanned; of the one behind it
     // where the thread's next pieces are: a tile further after every access
     const size_t tok = tok0 + from + row;
     const char *x_at = static_cast<const char *>(p.x) + (tok * p.x_stride + ch0) * ES, *dt_at = static_cast<const char *>(p.dt) + (tok * p.dt_stride + ch0) * ES;
     const char *z_at = static_cast<const char *>(p.z) + (tok * p.z_stride + ch0) * ES, *bc_at = static_cast<const char *>(bc) + ((tok0 + from + brow) * bc_stride + bcol % N) * ES;
     char *y_at = static_cast<char *>(p.y) + (tok * p.y_stride + ch0) * ES;
-    auto fetch = [&](int t0) {
+    auto fetch = [&](Fetched &f, int t0) {
+        if (t0 >= len) return;
         const int n = t0 + row < len ? live : 0;                                  // what lies behind a sequence's tokens is not read
-        nx.load(x_at, n);
-        ndt.load(dt_at, n);
-        if (OUT && p.z) nz.load(z_at, n);
+        f.x.load(x_at, n);
+        f.dt.load(dt_at, n);
+        if (OUT && p.z) f.z.load(z_at, n);
         const bool there = t0 + brow < len && (OUT || !is_c);
 #pragma unroll
-        for (int i = 0; i < BCW; ++i) nbc[i] = there ? reinterpret_cast<const uint32_t *>(bc_at)[i] : 0u;
+        for (int i = 0; i < BCW; ++i) f.bc[i] = there ? reinterpret_cast<const uint32_t *>(bc_at)[i] : 0u;
         x_at += T * ES * p.x_stride; dt_at += T * ES * p.dt_stride; z_at += T * ES * p.z_stride; bc_at += T * ES * bc_stride;
     };
-    auto prepare = [&](int t0, int buf) {
+    auto prepare = [&](const Fetched &f, int t0, int buf) {
         float2 in[CH];
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            float d = ndt.get(i);
+            float d = f.dt.get(i);
             if (p.softplus) d = softplus_exact(d + bias[i]);
             d = t0 + row < len ? d : 0.f;                                         // tokens that are none leave the state as it is
-            in[i] = make_float2(d, d * nx.get(i));
+            in[i] = make_float2(d, d * f.x.get(i));
         }
 #pragma unroll
         for (int i = 0; i < CH; i += 2) *reinterpret_cast<float4 *>(&sIn[buf][row][col + i]) = make_float4(in[i].x, in[i].y, in[i + 1].x, in[i + 1].y);
@@ -263,8 +267,8 @@ void selective_scan_kernel(const ScanParams p)
 #pragma unroll
             for (int i = 0; i < BC; i += 2) {
                 float2 v;
-                if constexpr (IO == SSMV_BF16) v = make_float2(__uint_as_float(nbc[i / 2] << 16), __uint_as_float(nbc[i / 2] & 0xffff0000u));
-                else v = make_float2(__uint_as_float(nbc[i]), __uint_as_float(nbc[i + 1]));
+                if constexpr (IO == SSMV_BF16) v = make_float2(__uint_as_float(f.bc[i / 2] << 16), __uint_as_float(f.bc[i / 2] & 0xffff0000u));
+                else v = make_float2(__uint_as_float(f.bc[i]), __uint_as_float(f.bc[i + 1]));
                 *reinterpret_cast<float2 *>(to + i) = v;
             }
         }
@@ -287,23 +291,30 @@ void selective_scan_kernel(const ScanParams p)
             for (int i = 0; i < CH; ++i) y[i] *= silu_fast(ez.get(i));
         store_piece<IO, CH>(to, y, live);
     };
+    fetch(even, from);
+    fetch(odd, from + T);
     if (from < len) {
-        fetch(from);
-        prepare(from, 0);
-        px = nx; pz = nz;
-        if (from + T < len) fetch(from + T);
+        prepare(even, from, 0);
+        px = even.x; pz = even.z;
+        fetch(even, from + 2 * T);
     }
     __syncthreads();
     int buf = 0, t0 = from;
-    for (; t0 < len; t0 += T, buf ^= 1) {                                         // beside the scan of the tile at t0
+    auto beside = [&](Fetched &f) {                                               // beside the scan of the tile at t0; f: of the next one
         if (t0 > from) finish(t0 - T, buf ^ 1);
         ex = px; ez = pz;
         if (t0 + T < len) {
-            prepare(t0 + T, buf ^ 1);
-            px = nx; pz = nz;
-            if (t0 + 2 * T < len) fetch(t0 + 2 * T);
+            prepare(f, t0 + T, buf ^ 1);
+            px = f.x; pz = f.z;
+            fetch(f, t0 + 3 * T);
         }
         __syncthreads();
+        t0 += T;
+        buf ^= 1;
+    };
+    while (t0 < len) {
+        beside(odd);
+        if (t0 < len) beside(even);
     }
     if (t0 > from) finish(t0 - T, buf ^ 1);
 }
