@@ -443,7 +443,7 @@ int ssm_selective_step(const ssmv_token_args *args, void *hip_stream);
  *   scores[r] + logits[r][v] - logsumexp(logits[r])     (differences and sums of candidates in 64 bits),
  * the beams_out best, best first; equal scores by the lower row, inside a row by the higher logit, then the lower token.
  * parent holds rows of the whole batch (sequence * beams_in + beam), ready to be the src_row of the next step's calls.
- *   - done (device int32 [batch*beams_in], or NULL): a row with done != 0 is a finished hypothesis: its logits are not read, its
+ *   - done (device int32 [batch*beams_in], or NULL): a row with done != 0 is a finished hypothesis: its logits do not count, its
  *     one candidate is itself, token `eos` with its score unchanged (further places of it: eos with score -inf).  done_out
  *     (or NULL): 1 where the parent was finished or the token is eos.
  *   - a logit of -inf (or NaN) is a token that is not allowed: score -inf, chosen only where nothing else is left, also where

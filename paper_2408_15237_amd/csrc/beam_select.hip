@@ -22,6 +22,50 @@ __device__ __forceinline__ float key_logit(Key k)
 }
 __device__ __forceinline__ unsigned key_token(Key k) { return 0xffffffffu - (unsigned)k; }
 
+// v combined with the lanes 1, 2, 4, .. apart (lanes of each other half, until `size` lanes agree), without a trip through LDS
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true)); }
+template <typename F>
+__device__ __forceinline__ float combine(float v, int size, F &&f)
+{
+    v = f(v, dpp<0xB1>(v));                                                       // the other lane of a pair, the other pair of a quad
+    v = f(v, dpp<0x4E>(v));
+    if (size >= 8) v = f(v, dpp<0x141>(v));                                       // mirrored in 8, in 16
+    if (size >= 16) v = f(v, dpp<0x140>(v));
+    if (size >= 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    if (size >= 64) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    return v;
+}
+// the sum over the wave, in 64 bits
+__device__ __forceinline__ double wave_sum64(double v)
+{
+    auto both = [&](auto &&move) {
+        const unsigned long long b = __builtin_bit_cast(unsigned long long, v);
+        const unsigned lo = __float_as_uint(move(__uint_as_float((unsigned)b))), hi = __float_as_uint(move(__uint_as_float((unsigned)(b >> 32))));
+        v += __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
+    };
+    both([](float x) { return dpp<0xB1>(x); });
+    both([](float x) { return dpp<0x4E>(x); });
+    both([](float x) { return dpp<0x141>(x); });
+    both([](float x) { return dpp<0x140>(x); });
+    auto swapped = [&](auto &&swap) {
+        const unsigned long long b = __builtin_bit_cast(unsigned long long, v);
+        const auto lo = swap((unsigned)b), hi = swap((unsigned)(b >> 32));
+        v = __builtin_bit_cast(double, (unsigned long long)hi[0] << 32 | lo[0]) + __builtin_bit_cast(double, (unsigned long long)hi[1] << 32 | lo[1]);
+    };
+    swapped([](unsigned x) { return __builtin_amdgcn_permlane16_swap(x, x, false, false); });
+    swapped([](unsigned x) { return __builtin_amdgcn_permlane32_swap(x, x, false, false); });
+    return v;
+}
+__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ float sum_of(float a, float b) { return a + b; }
+
 constexpr int THREADS = 256, WAVES = THREADS / 64;
 constexpr int kList = 1024;                                                       // candidates that the short way of a piece may collect
 
@@ -46,7 +90,7 @@ __global__ __launch_bounds__(THREADS) void beam_piece_kernel(const BeamParams p)
     const unsigned tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
     const int piece = blockIdx.x, keep = p.keep;
     const size_t row = blockIdx.y;
-    if (p.done && p.done[row] != 0) return;                                       // a finished row's logits are not read
+    const int done = p.done ? p.done[row] : 0;
     const char *base = static_cast<const char *>(p.logits) + row * p.row_stride * ES;
     Key *out = p.keys + (row * p.pieces + piece) * keep;
     const int size = keep <= 4 ? 64 : keep <= 8 ? 32 : keep <= 16 ? 16 : keep <= 32 ? 8 : 4, groups = THREADS / size;
@@ -64,6 +108,7 @@ __global__ __launch_bounds__(THREADS) void beam_piece_kernel(const BeamParams p)
         }
     };
     if (end >= EV) fetch(begin);
+    if (done != 0) return;                                                        // a finished row: known by when the first logits are on their way
     if (tid == 0) sCount = 0;
     // the places of the list's first `count` keys: a quad of lanes to a key
     auto rank = [&](int count, Key *to) {
@@ -103,8 +148,7 @@ __global__ __launch_bounds__(THREADS) void beam_piece_kernel(const BeamParams p)
         float most = -INFINITY;                                                   // (the maximum of a number and NaN is the number)
 #pragma unroll
         for (int i = 0; i < E; ++i) most = fmaxf(most, v[i]);
-        float group = most;
-        for (int o = 1; o < size; o *= 2) group = fmaxf(group, __shfl_xor(group, o));
+        const float group = combine(most, size, larger);
         if (tid % size == 0) sMax[tid / size] = group;
         __syncthreads();
         const float before = m;
@@ -170,9 +214,7 @@ __global__ __launch_bounds__(THREADS) void beam_piece_kernel(const BeamParams p)
         }
         const bool final = chunk + 1 == p.chunks;
         if (final) {
-            float all = sum;
-#pragma unroll
-            for (int o = 32; o > 0; o /= 2) all += __shfl_xor(all, o);
+            const float all = combine(sum, 64, sum_of);
             if (lane == 0) sSum[wave] = all;
         }
         __syncthreads();
@@ -225,30 +267,35 @@ __global__ __launch_bounds__(THREADS) void beam_piece_kernel(const BeamParams p)
     }
 }
 
-// A workgroup per sequence.  A wave per row merges the pieces: the largest of the lists' last keys is a bound that `keep` candidates reach,
+// A workgroup per sequence.  A wave per row merges the pieces: the largest of the lists' last logits is a bound that `keep` candidates reach,
 // what reaches it is moved together, and its places are counted.  Then the rows of the sequence in the same way, by their scores: equal
 // ones by their places, which are in the order of row and rank.
 __global__ __launch_bounds__(1024) void beam_merge_kernel(const BeamParams p)
 {
-    __shared__ Key sLists[kMergeKeys];
+    constexpr int KEYS = 4;                                                       // of a lane at a time
+    __shared__ __attribute__((aligned(16))) Key sLists[kMergeKeys];
     __shared__ double sScore[SSMV_BEAMS_MAX * SSMV_BEAMS_MAX];
     __shared__ int sToken[SSMV_BEAMS_MAX * SSMV_BEAMS_MAX], sDone[SSMV_BEAMS_MAX];
     __shared__ int sCount;
     const unsigned tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6, waves = blockDim.x >> 6;
     const int W = p.beams_in, keep = p.keep, pieces = p.pieces, n = pieces * keep;
     const size_t row0 = (size_t)blockIdx.x * W;
-    Key *list = sLists + (size_t)wave * n;
+    Key *list = sLists + (size_t)wave * merge_room(n);
     if (tid == 0) sCount = 0;
     for (int r = wave; r < W; r += waves) {
         const size_t row = row0 + r;
         const Key *from = p.keys + row * n;
         // all that the row needs of memory at once, also where it turns out to be finished
         const float2 part = (int)lane < pieces ? p.sums[row * pieces + lane] : make_float2(-kTop, 0.f);      // at most 64 pieces
-        Key bound = (int)lane < pieces ? from[lane * keep + keep - 1] : 0;
+        const Key worst = (int)lane < pieces ? from[lane * keep + keep - 1] : 0;
+        Key k[KEYS];
+        auto fetch = [&](int i0) {
+#pragma unroll
+            for (int u = 0; u < KEYS; ++u) k[u] = i0 + u * 64 + (int)lane < n ? from[i0 + u * 64 + lane] : 0;
+        };
+        fetch(0);
         const int done = p.done ? p.done[row] : 0;
         float given = p.scores[row];
-#pragma unroll 4
-        for (int i = lane; i < n; i += 64) list[i] = from[i];
         given = given != given ? -INFINITY : fminf(given, kTop);
         if (lane == 0) sDone[r] = done;
         if (done != 0) {
@@ -258,35 +305,32 @@ __global__ __launch_bounds__(1024) void beam_merge_kernel(const BeamParams p)
             }
             continue;
         }
-        float m = part.x;
-        for (int o = 1; o < pieces; o *= 2) {
-            m = fmaxf(m, __shfl_xor(m, o));
-            const Key other = __shfl_xor(bound, o);
-            bound = other > bound ? other : bound;
-        }
-        m = __shfl(m, 0);
-        bound = __shfl(bound, 0);
-        double s = (double)part.y * (double)__builtin_amdgcn_exp2f((part.x - m) * 1.4426950408889634f);
-        for (int o = 1; o < pieces; o *= 2) s += __shfl_xor(s, o);
-        const double lse = log(__shfl(s, 0));
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");                    // the list is this wave's own
+        const float m = combine(part.x, 64, larger), bound = combine(worst ? key_logit(worst) : -INFINITY, 64, larger);
+        const double lse = log(wave_sum64((double)part.y * (double)__builtin_amdgcn_exp2f((part.x - m) * 1.4426950408889634f)));
         int count = 0;
-        for (int i0 = 0; i0 < n; i0 += 64) {                                      // a candidate moves down, never past one not looked at
-            const Key k = i0 + (int)lane < n ? list[i0 + lane] : 0;
-            const bool in = k != 0 && k >= bound;
-            const unsigned long long mask = __ballot(in);
-            if (in) list[count + __builtin_popcountll(mask & ((1ull << lane) - 1))] = k;
-            count += __builtin_popcountll(mask);
+        for (int i0 = 0; i0 < n; i0 += 64 * KEYS) {
+            if (i0 > 0) fetch(i0);
+#pragma unroll
+            for (int u = 0; u < KEYS; ++u) {
+                const bool in = k[u] != 0 && key_logit(k[u]) >= bound;
+                const unsigned long long mask = __ballot(in);
+                if (in) list[count + __builtin_popcountll(mask & ((1ull << lane) - 1))] = k[u];
+                count += __builtin_popcountll(mask);
+            }
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (lane == 0) list[count] = 0;                                           // they are read in pairs
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");                    // the list is this wave's own
         for (int i = lane; i < count; i += 64) {
-            const Key k = list[i];
+            const Key own = list[i];
             int rank = 0;
-#pragma unroll 8
-            for (int j = 0; j < count; ++j) rank += list[j] > k;
+#pragma unroll 4
+            for (int j = 0; j < count; j += 2) {
+                const ulonglong2 two = *reinterpret_cast<const ulonglong2 *>(list + j);
+                rank += (two.x > own) + (two.y > own);
+            }
             if (rank < keep) {
-                const float l = key_logit(k);
-                sToken[r * keep + rank] = (int)key_token(k);
+                const float l = key_logit(own);
+                sToken[r * keep + rank] = (int)key_token(own);
                 sScore[r * keep + rank] = l == -INFINITY ? -INFINITY : (double)given + ((double)l - (double)m - lse);
             }
         }
@@ -335,7 +379,7 @@ int launch_beam_select(const BeamParams &p, hipStream_t stream)
     }
     const int e = (int)hipGetLastError();
     if (e != 0) return e;
-    int waves = kMergeKeys / (p.pieces * p.keep);                                           // at least 4 (beam_plan)
+    int waves = kMergeKeys / merge_room(p.pieces * p.keep);                                 // at least 3 (beam_plan)
     waves = waves < 16 ? waves : 16;
     const int wanted = p.beams_in > 4 ? p.beams_in : 4;
     hipLaunchKernelGGL(beam_merge_kernel, dim3((unsigned)p.batch), dim3(64 * (waves < wanted ? waves : wanted)), 0, stream, p);

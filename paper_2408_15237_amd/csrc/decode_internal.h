@@ -111,7 +111,8 @@ inline ScanPlan scan_plan(int batch, int C, int N, int L)
 }
 
 constexpr int kSmallKeep = 16;       // candidates of a small piece at most
-constexpr int kMergeKeys = 8192;     // keys that the merge of a sequence has room for: of four rows at least
+constexpr int kMergeKeys = 8192;     // keys that the merge of a sequence has room for: of three rows at least
+__host__ __device__ constexpr int merge_room(int n) { return (n + 2) / 2 * 2; }    // of a row's n: pairs, and a place behind the last
 
 struct BeamPlan {
     int small;               // 1: chunks of 2048 logits, 0: of 8192
