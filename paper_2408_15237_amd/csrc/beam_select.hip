@@ -26,19 +26,19 @@ __device__ __forceinline__ unsigned key_token(Key k) { return 0xffffffffu - (uns
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true)); }
 template <typename F>
-__device__ __forceinline__ float combine(float v, int size, F &&f)
+__device__ __forceinline__ float combine(float v, int size, F &&f)                // f(one, other, how many lanes apart)
 {
-    v = f(v, dpp<0xB1>(v));                                                       // the other lane of a pair, the other pair of a quad
-    v = f(v, dpp<0x4E>(v));
-    if (size >= 8) v = f(v, dpp<0x141>(v));                                       // mirrored in 8, in 16
-    if (size >= 16) v = f(v, dpp<0x140>(v));
+    v = f(v, dpp<0xB1>(v), 1);                                                    // the other lane of a pair, the other pair of a quad
+    v = f(v, dpp<0x4E>(v), 2);
+    if (size >= 8) v = f(v, dpp<0x141>(v), 4);                                    // mirrored in 8, in 16
+    if (size >= 16) v = f(v, dpp<0x140>(v), 8);
     if (size >= 32) {
         const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-        v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+        v = f(__uint_as_float(r[0]), __uint_as_float(r[1]), 16);
     }
     if (size >= 64) {
         const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-        v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+        v = f(__uint_as_float(r[0]), __uint_as_float(r[1]), 32);
     }
     return v;
 }
@@ -63,8 +63,8 @@ __device__ __forceinline__ double wave_sum64(double v)
     swapped([](unsigned x) { return __builtin_amdgcn_permlane32_swap(x, x, false, false); });
     return v;
 }
-__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
-__device__ __forceinline__ float sum_of(float a, float b) { return a + b; }
+__device__ __forceinline__ float larger(float a, float b, int) { return fmaxf(a, b); }
+__device__ __forceinline__ float sum_of(float a, float b, int) { return a + b; }
 
 constexpr int THREADS = 256, WAVES = THREADS / 64;
 constexpr int kList = 1024;                                                       // candidates that the short way of a piece may collect
@@ -231,8 +231,9 @@ __global__ __launch_bounds__(THREADS) void beam_piece_kernel(const BeamParams p)
             if (tid == 0) sKey = 1;                                               // every candidate there is
             __syncthreads();
             int r = 0;
+            const int used = min(THREADS, (end - first + EV - 1) / EV);           // threads that have any
 #pragma unroll 8
-            for (int i = 0; i < THREADS; ++i) r += sThread[i] > best;
+            for (int i = 0; i < used; ++i) r += sThread[i] > best;
             if (best != 0 && r == keep - 1) sKey = best;                          // keys are unique: one thread
             if (tid == 0) sCount = held;
             __syncthreads();
@@ -267,8 +268,9 @@ __global__ __launch_bounds__(THREADS) void beam_piece_kernel(const BeamParams p)
     }
 }
 
-// A workgroup per sequence.  A wave per row merges the pieces: the largest of the lists' last logits is a bound that `keep` candidates reach,
-// what reaches it is moved together, and its places are counted.  Then the rows of the sequence in the same way, by their scores: equal
+// A workgroup per sequence.  A wave per row merges the pieces.  The largest of the lists' last logits is a bound that `keep` candidates
+// reach; so is, of at least `keep` groups of lists, the least of the groups' best.  What reaches both is moved together, and its
+// places are counted.  Then the rows of the sequence in the same way, by their scores: equal
 // ones by their places, which are in the order of row and rank.
 __global__ __launch_bounds__(1024) void beam_merge_kernel(const BeamParams p)
 {
@@ -281,6 +283,8 @@ __global__ __launch_bounds__(1024) void beam_merge_kernel(const BeamParams p)
     const int W = p.beams_in, keep = p.keep, pieces = p.pieces, n = pieces * keep;
     const size_t row0 = (size_t)blockIdx.x * W;
     Key *list = sLists + (size_t)wave * merge_room(n);
+    // groups of lanes, at least `keep`, and the lists that are spread over the lanes: both powers of two
+    const int groups = keep > 1 ? 1 << (32 - __builtin_clz(keep - 1)) : 1, spread = 1 << (31 - __builtin_clz(pieces));
     if (tid == 0) sCount = 0;
     for (int r = wave; r < W; r += waves) {
         const size_t row = row0 + r;
@@ -288,6 +292,12 @@ __global__ __launch_bounds__(1024) void beam_merge_kernel(const BeamParams p)
         // all that the row needs of memory at once, also where it turns out to be finished
         const float2 part = (int)lane < pieces ? p.sums[row * pieces + lane] : make_float2(-kTop, 0.f);      // at most 64 pieces
         const Key worst = (int)lane < pieces ? from[lane * keep + keep - 1] : 0;
+        Key first = 0, second = 0;                                                // the best of the lane's lists: adjacent lanes have the same or adjacent ones
+        if (groups <= spread) {
+            const int at = lane * spread / 64;
+            first = from[at * keep];
+            if (at + spread < pieces) second = from[(at + spread) * keep];
+        }
         Key k[KEYS];
         auto fetch = [&](int i0) {
 #pragma unroll
@@ -305,7 +315,10 @@ __global__ __launch_bounds__(1024) void beam_merge_kernel(const BeamParams p)
             }
             continue;
         }
-        const float m = combine(part.x, 64, larger), bound = combine(worst ? key_logit(worst) : -INFINITY, 64, larger);
+        const float m = combine(part.x, 64, larger);
+        float bound = combine(worst ? key_logit(worst) : -INFINITY, 64, larger);
+        const float best = fmaxf(first ? key_logit(first) : -INFINITY, second ? key_logit(second) : -INFINITY);
+        bound = fmaxf(bound, combine(best, 64, [&](float a, float b, int apart) { return apart * groups < 64 ? fmaxf(a, b) : fminf(a, b); }));
         const double lse = log(wave_sum64((double)part.y * (double)__builtin_amdgcn_exp2f((part.x - m) * 1.4426950408889634f)));
         int count = 0;
         for (int i0 = 0; i0 < n; i0 += 64 * KEYS) {
