@@ -138,7 +138,11 @@ __global__ __launch_bounds__(THREADS) void beam_piece_kernel(const BeamParams p)
             }
             if (first + CHUNK > end) {
 #pragma unroll
-                for (int i = 0; i < E; ++i) v[i] = there(i) ? v[i] : -INFINITY;
+                for (int i = 0; i < E; i += EV)
+                    if (place(i) > end - EV) {
+#pragma unroll
+                        for (int j = i; j < i + EV; ++j) v[j] = there(j) ? v[j] : -INFINITY;
+                    }
             }
             if (chunk + 1 < p.chunks) fetch(first + CHUNK);
         } else {                                                                  // a vocabulary of less than one vector
