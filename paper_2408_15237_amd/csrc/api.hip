@@ -668,8 +668,8 @@ int ssm_causal_conv(const ssmv_conv_args *args, void *hip_stream)
     if (a.src_row && a.conv_out && a.conv_out == a.conv_in) return fail(SSMV_EINVAL, "conv_out may be conv_in only without src_row");
     if (a.batch > 65535) return fail(SSMV_EUNSUPPORTED, "batch %d > 65535", a.batch);
     if ((double)a.batch * a.L * a.channels > 2.0e11) return fail(SSMV_EUNSUPPORTED, "more than 2e11 values");     // 32 bits count the workgroups
-    // a sequence's tiles of at least 8 tokens, counted with 32 bits where every channel has a thread
-    if (((double)a.L / 8 + 1) * a.channels > 2.1e9) return fail(SSMV_EUNSUPPORTED, "a sequence of %d tokens x %d channels: feed it in pieces", a.L, a.channels);
+    // a sequence's tiles of at least 4 tokens, counted with 32 bits where every channel has a thread
+    if (((double)a.L / 4 + 1) * (a.channels > 8 ? a.channels : 8) > 2.1e9) return fail(SSMV_EUNSUPPORTED, "a sequence of %d tokens x %d channels: feed it in pieces", a.L, a.channels);
     CausalConvParams p{};
     p.x = a.x; p.wgt = a.wgt; p.bias = a.bias; p.conv_in = a.conv_in; p.src_row = a.src_row; p.seq_len = a.seq_len; p.out = a.out; p.conv_out = a.conv_out;
     p.x_stride = a.x_stride; p.out_stride = a.out_stride;

@@ -56,6 +56,7 @@ struct Chunk {
     }
 };
 
+// Bound by memory: a token row in, a token row out (8 x 2048 x 5120 bf16, 336 MB: 54.7 us, 6.1 TB/s; a copy of 1 GB 5.1 to 6.1).
 // A thread owns VEC adjacent channels of T tokens: it requests its tokens and the three before them together, and slides over
 // them in registers.  The three are those of the thread of the tokens before, 2^lanes threads ahead in the same workgroup but for one
 // tile in 256 / 2^lanes, so that they come out of the L1 and what a workgroup reads does not depend on where others run.  The first tokens
@@ -157,9 +158,12 @@ int launch(const CausalConvParams &p, hipStream_t stream)
     // Whatever comes next reads the outputs: they go through the caches as long as those can hold them (256 MB behind the L2s, which the
     // inputs pass too).  Conv and a sum over its outputs, us, through / past the caches: 34 MB 56.0 / 63.7, 84 MB 122.8 / 129.1,
     // 168 MB 277.7 / 270.4.
+    // Four tokens of a thread: more of them in flight than with eight (us, 8 / 4: 100 x 8192 5.8 / 4.5, 2048 x 8192 14.7 / 13.9, 8 x 2048 x 5120
+    // 62.4 / 60.8), but for large fp32 launches, which have enough of them (4 x 2048 x 8192: 95.7 / 99.5).
+    constexpr int LONG = IO == SSMV_F32 ? 8 : 4;
     if constexpr (VEC > 1)
-        if ((size_t)p.batch * p.L * p.C * Chunk<IO, VEC>::ES > (128u << 20)) return go(causal_conv_kernel<IO, VEC, 8, true>, 8);
-    return go(causal_conv_kernel<IO, VEC, 8, false>, 8);
+        if ((size_t)p.batch * p.L * p.C * Chunk<IO, VEC>::ES > (128u << 20)) return go(causal_conv_kernel<IO, VEC, LONG, true>, LONG);
+    return go(causal_conv_kernel<IO, VEC, 4, false>, 4);
 }
 
 // a thread per element of conv_out

@@ -108,12 +108,20 @@ __device__ __forceinline__ float fold16(float a, float b)
 
 constexpr int kScanWaves = 4, kHelpWaves = 4;
 
+// h <- exp(dt' A) h + (dt' x) B,  y = C.h + D x: five operations and an exponential for every channel, token and state index, against 8 bytes
+// (bf16, gated) for all N indices of a channel and token.  So the vector units bound it: an operation takes a wave 4 cycles, exp2 8, 24 in all;
+// A and exp(dt' A) differ in every lane, which leaves the matrix cores nothing to contract but y, one useful column of sixteen.
+//
 // A workgroup takes CHW channels of a sequence, T tokens at a time.  Four of its waves scan: a lane per channel and S of the N state
 // indices, which stay in registers from the first token to the last; with fewer than 64 channels the 64 / CHW parts of a wave take
 // other indices of the same channels.  Four waves help: each of their threads owns CH adjacent channels of one token of a
 // tile, prepares (dt', dt' x) of the tile ahead of the scan, and of the tile behind it sums the partial outputs, adds the skip, gates
 // and stores, so that a tile's three stages run side by side and one barrier a tile is enough.  Everything changes hands in LDS.
-// B of a token is a broadcast operand: 16 / S tokens' worth sit in the lanes of every 16 of a register.
+// B of a token is a broadcast operand of the multiplication (16 / S tokens' worth sit in the lanes of every 16 of a register); as scalar
+// registers B and C cost waits and unpacking on the scalar unit (522 us for 1 x 2048 x 8192 x 16, then in two barriers a tile, 225 with the broadcast).
+// Measured, bf16, softplus and gate, us: 16 x 2048 x 8192 x 16 909, which is 34 cycles of a SIMD for 64 values of h (24 the recurrence, 3 its LDS
+// accesses, 7 the helpers); 1 x 2048 x 8192 88 (64 workgroups' waves of 64 channels: 152; a second pass over segments: 114); 1 x 2048 x 1536
+// 31 (in one segment 65); 8 x 2048 x 8192 x 64 1483.
 // OUT false: only the state at the segment's end and the sum of its steps, of all segments but the last.
 template <int IO, int N, int CHW, bool OUT>
 __global__ __launch_bounds__(64 * (kScanWaves + kHelpWaves)) __attribute__((amdgpu_waves_per_eu(4)))
