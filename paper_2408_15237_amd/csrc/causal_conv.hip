@@ -56,7 +56,7 @@ struct Chunk {
     }
 };
 
-// Bound by memory: a token row in, a token row out (8 x 2048 x 5120 bf16, 336 MB: 54.7 us, 6.1 TB/s; a copy of 1 GB 5.1 to 6.1).
+// Bound by memory: a token row in, a token row out (8 x 2048 x 5120 bf16, 336 MB, other tensors in every call: 60.8 us, 5.5 TB/s; copies of 1 GB 5.1 to 6.1).
 // A thread owns VEC adjacent channels of T tokens: it requests its tokens and the three before them together, and slides over
 // them in registers.  The three are those of the thread of the tokens before, 2^lanes threads ahead in the same workgroup but for one
 // tile in 256 / 2^lanes, so that they come out of the L1 and what a workgroup reads does not depend on where others run.  The first tokens

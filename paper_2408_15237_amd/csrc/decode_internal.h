@@ -82,8 +82,9 @@ struct ScanPlan {
 // token a workgroup that has a compute unit to itself takes lone = 15 + N ns (16 channels), 18 + 1.6 N (32), 35 + 2.6 N (64); a compute
 // unit with k of them takes k times 14 + 0.75 N, 15 + 1.3 N, 22 + 2.5 N where that is more.  A cut prompt costs a pass over all
 // segments but the last that forms their end states (0.65 of a full pass), and 5 us.
-// (us, N = 16, 2048 tokens, 64 / 32 / 16 channels: 1 x 8192 152 / 91 / 105; 1 x 1536 151 / 81 / 65, in 8 segments 42 / 37 / 37;
-//  8 x 5120 380 / 360 / 445; 16 x 8192 953 / 1088 / 1385, and 1606 / 1825 / 2248 in 8 segments.)
+// (us, N = 16, 2048 tokens, 64 / 32 / 16 channels: 1 x 8192 140 / 79 / 91, in 8 segments 106 / 112 / 139; 1 x 1536 137 / 78 / 55, in 16 segments
+//  36 / 30 / 37; 8 x 5120 342 / 334 / 427; 16 x 8192 909 / 1045 / 1336, in 8 segments 1481 / 1732 / 2131.  Over 20 shapes, of 1 to 32 sequences,
+//  64 to 8192 channels and all N, its choice is within 6 % of the best of 24, noise included, but for 10 % once.)
 inline ScanPlan scan_plan(int batch, int C, int N, int L)
 {
     const int tiles = (L + kScanTile - 1) / kScanTile;

@@ -120,8 +120,8 @@ constexpr int kScanWaves = 4, kHelpWaves = 4;
 // B of a token is a broadcast operand of the multiplication (16 / S tokens' worth sit in the lanes of every 16 of a register); as scalar
 // registers B and C cost waits and unpacking on the scalar unit (522 us for 1 x 2048 x 8192 x 16, then in two barriers a tile, 225 with the broadcast).
 // Measured, bf16, softplus and gate, us: 16 x 2048 x 8192 x 16 909, which is 34 cycles of a SIMD for 64 values of h (24 the recurrence, 3 its LDS
-// accesses, 7 the helpers); 1 x 2048 x 8192 88 (64 workgroups' waves of 64 channels: 152; a second pass over segments: 114); 1 x 2048 x 1536
-// 31 (in one segment 65); 8 x 2048 x 8192 x 64 1483.
+// accesses, 7 the helpers); 1 x 2048 x 8192 79 (in workgroups of 64 channels 140, those in 8 segments 106); 1 x 2048 x 1536 30 (in one
+// segment 55); 8 x 2048 x 8192 x 64 1483.
 // OUT false: only the state at the segment's end and the sum of its steps, of all segments but the last.
 template <int IO, int N, int CHW, bool OUT>
 __global__ __launch_bounds__(64 * (kScanWaves + kHelpWaves)) __attribute__((amdgpu_waves_per_eu(4)))
@@ -180,7 +180,7 @@ void selective_scan_kernel(const ScanParams p)
         for (int t0 = from, buf = 0; t0 < len; t0 += T, buf ^= 1) {
             const int n = min(len - t0, T);
             // U tokens at a time.  Of a whole tile the operands of the next U are requested ahead of the arithmetic on these where a lane has
-            // few states: one wave a SIMD then waits for LDS otherwise (1 x 2048 x 8192 x 16: 92.9 -> 87.9 us).  With four states and
+            // few states: one wave a SIMD then waits for LDS otherwise (1 x 2048 x 8192 x 16: 92.9 -> 88.3 us).  With four states and
             // several waves a SIMD the registers that it takes cost more (16 x 2048 x 8192: 910 -> 936).
             struct Block {
                 float2 in[U];
