@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 from typing import Dict, List, Optional
 
@@ -54,8 +55,11 @@ class ssmv_prefill_args(ctypes.Structure):
 
 
 def _args_struct(name, pointers, longs, ints):
-    return type(name, (ctypes.Structure,), {"_fields_": [(n, ctypes.c_void_p) for n in pointers] + [(n, ctypes.c_int64) for n in longs] +
-                                            [(n, ctypes.c_int32) for n in ints]})
+    """The ctypes form of an argument struct; `pack` makes its bytes from the fields' values in half the time."""
+    cls = type(name, (ctypes.Structure,), {"_fields_": [(n, ctypes.c_void_p) for n in pointers] + [(n, ctypes.c_int64) for n in longs] +
+                                           [(n, ctypes.c_int32) for n in ints]})
+    cls.pack = struct.Struct("%dP%dq%di0P" % (len(pointers), len(longs), len(ints))).pack        # 0P: padded like the C struct
+    return cls
 
 
 ssmv_conv_args = _args_struct("ssmv_conv_args", ("x", "wgt", "bias", "conv_in", "src_row", "seq_len", "out", "conv_out"), ("x_stride", "out_stride"),
@@ -68,6 +72,9 @@ ssmv_token_args = _args_struct("ssmv_token_args", ("x", "dt", "dt_bias", "A", "B
                                ("rows", "rows_in", "nheads", "headdim", "dstate", "ngroups", "io_dtype", "a_mode", "dt_softplus"))
 ssmv_beam_args = _args_struct("ssmv_beam_args", ("logits", "scores", "done", "parent", "token", "scores_out", "done_out", "workspace"), ("row_stride",),
                               ("batch", "beams_in", "beams_out", "vocab", "io_dtype", "eos"))
+
+
+_pack_conv, _pack_scan, _pack_token, _pack_beam = ssmv_conv_args.pack, ssmv_scan_args.pack, ssmv_token_args.pack, ssmv_beam_args.pack
 
 
 class SsmvError(RuntimeError):
@@ -100,7 +107,6 @@ class ssmv_cache(ctypes.Structure):
 
 
 _lib = None
-_byref = ctypes.byref
 
 
 def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
@@ -132,9 +138,8 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.ssmv_materialize_block.argtypes = [dp, cp, vp, vp, i32, vp, vp]
     lib.ssmv_first_conflict.argtypes = [vp, vp, i32, i32, vp, vp]
     lib.ssmv_gated_rmsnorm.argtypes = [vp, vp, vp, i32, i32, i32, ctypes.c_float, i32, vp, vp]
-    for name, args in (("ssm_causal_conv", ssmv_conv_args), ("ssm_selective_scan", ssmv_scan_args), ("ssm_selective_step", ssmv_token_args),
-                       ("ssmv_beam_select", ssmv_beam_args)):
-        getattr(lib, name).argtypes = [ctypes.POINTER(args), vp]
+    for name in ("ssm_causal_conv", "ssm_selective_scan", "ssm_selective_step", "ssmv_beam_select"):          # a packed struct, a stream
+        getattr(lib, name).argtypes = [vp, vp]
     lib.ssm_selective_scan_workspace.argtypes = [i32, i32, i32, i32, ctypes.POINTER(sz)]
     lib.ssmv_beam_workspace.argtypes = [i32, i32, i32, i32, ctypes.POINTER(sz)]
     lib.ssmv_conv_history.argtypes = [dp, cp, vp, vp]
@@ -284,6 +289,11 @@ def ssmv_gated_rmsnorm(y, z, weight, rows: int, channels: int, group_size: int, 
 
 # ---- plain and beam decoding: from state to state -----------------------------------------------------------------------
 
+def _ptrs(*tensors):
+    """_ptr of several arguments, with 0 for None."""
+    return [0 if t is None else t if t.__class__ is int else t.data_ptr() for t in tensors]
+
+
 def _rows(t, rows_in, src_row) -> int:
     """Rows of the state that goes in: as given, else the tensor's first dimension where an index looks at them, else 0 (as many as go out)."""
     return rows_in or (0 if src_row is None or t is None or isinstance(t, int) else t.shape[0])
@@ -291,9 +301,9 @@ def _rows(t, rows_in, src_row) -> int:
 
 def ssm_causal_conv(*, x, wgt, out, batch: int, channels: int, L: int, io, bias=None, act="none", conv_in=None, conv_out=None, src_row=None,
                     rows_in: int = 0, seq_len=None, x_stride: int = 0, out_stride: int = 0, stream=None) -> None:
-    a = ssmv_conv_args(_ptr(x), _ptr(wgt), _ptr(bias), _ptr(conv_in), _ptr(src_row), _ptr(seq_len), _ptr(out), _ptr(conv_out), x_stride, out_stride,
-                       batch, _rows(conv_in, rows_in, src_row), channels, L, IO_CODES.get(io, io), ACT_CODES.get(act, act))
-    _ck((_lib or load_library()).ssm_causal_conv(_byref(a), _stream(stream)))
+    a = _pack_conv(*_ptrs(x, wgt, bias, conv_in, src_row, seq_len, out, conv_out), x_stride, out_stride, batch, _rows(conv_in, rows_in, src_row),
+                   channels, L, IO_CODES.get(io, io), ACT_CODES.get(act, act))
+    _ck((_lib or load_library()).ssm_causal_conv(a, _stream(stream)))
 
 
 def ssm_selective_scan_workspace(batch: int, channels: int, dstate: int, L: int) -> int:
@@ -305,19 +315,17 @@ def ssm_selective_scan_workspace(batch: int, channels: int, dstate: int, L: int)
 def ssm_selective_scan(*, x, dt, A, Bm, Cm, D, y_out, batch: int, channels: int, dstate: int, L: int, io, dt_bias=None, dt_softplus: bool = False,
                        z=None, h_in=None, h_out=None, src_row=None, rows_in: int = 0, seq_len=None, x_stride: int = 0, dt_stride: int = 0,
                        b_stride: int = 0, c_stride: int = 0, z_stride: int = 0, y_stride: int = 0, workspace=None, stream=None) -> None:
-    a = ssmv_scan_args(_ptr(x), _ptr(dt), _ptr(dt_bias), _ptr(A), _ptr(Bm), _ptr(Cm), _ptr(D), _ptr(z), _ptr(h_in), _ptr(src_row), _ptr(seq_len),
-                       _ptr(y_out), _ptr(h_out), _ptr(workspace), x_stride, dt_stride, b_stride, c_stride, z_stride, y_stride,
-                       batch, _rows(h_in, rows_in, src_row), channels, dstate, L, IO_CODES.get(io, io), dt_softplus)
-    _ck((_lib or load_library()).ssm_selective_scan(_byref(a), _stream(stream)))
+    a = _pack_scan(*_ptrs(x, dt, dt_bias, A, Bm, Cm, D, z, h_in, src_row, seq_len, y_out, h_out, workspace), x_stride, dt_stride, b_stride, c_stride,
+                   z_stride, y_stride, batch, _rows(h_in, rows_in, src_row), channels, dstate, L, IO_CODES.get(io, io), dt_softplus)
+    _ck((_lib or load_library()).ssm_selective_scan(a, _stream(stream)))
 
 
 def ssm_selective_step(*, x, dt, A, Bm, Cm, D, y_out, h_in, h_out, rows: int, nheads: int, headdim: int, dstate: int, io, ngroups: int = 1,
                        a_mode="scalar", dt_bias=None, dt_softplus: bool = False, z=None, src_row=None, rows_in: int = 0, x_stride: int = 0,
                        dt_stride: int = 0, b_stride: int = 0, c_stride: int = 0, z_stride: int = 0, y_stride: int = 0, stream=None) -> None:
-    a = ssmv_token_args(_ptr(x), _ptr(dt), _ptr(dt_bias), _ptr(A), _ptr(Bm), _ptr(Cm), _ptr(D), _ptr(z), _ptr(h_in), _ptr(src_row), _ptr(y_out),
-                        _ptr(h_out), x_stride, dt_stride, b_stride, c_stride, z_stride, y_stride, rows, _rows(h_in, rows_in, src_row),
-                        nheads, headdim, dstate, ngroups, IO_CODES.get(io, io), MODE_CODES.get(a_mode, a_mode), dt_softplus)
-    _ck((_lib or load_library()).ssm_selective_step(_byref(a), _stream(stream)))
+    a = _pack_token(*_ptrs(x, dt, dt_bias, A, Bm, Cm, D, z, h_in, src_row, y_out, h_out), x_stride, dt_stride, b_stride, c_stride, z_stride, y_stride,
+                    rows, _rows(h_in, rows_in, src_row), nheads, headdim, dstate, ngroups, IO_CODES.get(io, io), MODE_CODES.get(a_mode, a_mode), dt_softplus)
+    _ck((_lib or load_library()).ssm_selective_step(a, _stream(stream)))
 
 
 def ssmv_beam_workspace(batch: int, beams_in: int, beams_out: int, vocab: int) -> int:
@@ -328,9 +336,9 @@ def ssmv_beam_workspace(batch: int, beams_in: int, beams_out: int, vocab: int) -
 
 def ssmv_beam_select(*, logits, scores, parent, token, scores_out, batch: int, beams_in: int, beams_out: int, vocab: int, io, workspace,
                      row_stride: int = 0, done=None, done_out=None, eos: int = -1, stream=None) -> None:
-    a = ssmv_beam_args(_ptr(logits), _ptr(scores), _ptr(done), _ptr(parent), _ptr(token), _ptr(scores_out), _ptr(done_out), _ptr(workspace), row_stride,
-                       batch, beams_in, beams_out, vocab, IO_CODES.get(io, io), eos)
-    _ck((_lib or load_library()).ssmv_beam_select(_byref(a), _stream(stream)))
+    a = _pack_beam(*_ptrs(logits, scores, done, parent, token, scores_out, done_out, workspace), row_stride, batch, beams_in, beams_out, vocab,
+                   IO_CODES.get(io, io), eos)
+    _ck((_lib or load_library()).ssmv_beam_select(a, _stream(stream)))
 
 
 def ssmv_conv_history(dims, cache, conv_out, stream=None) -> None:

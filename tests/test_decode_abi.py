@@ -108,3 +108,12 @@ def test_workspaces():
     small, large = ssmv.ssmv_beam_workspace(1, 1, 1, 1), ssmv.ssmv_beam_workspace(16, 8, 8, 128011)
     assert 0 < small <= 256 and small < large < 1 << 22
     assert small % 16 == 0 and large % 16 == 0
+
+
+@pytest.mark.parametrize("name", ["ssmv_conv_args", "ssmv_scan_args", "ssmv_token_args", "ssmv_beam_args"])
+def test_packed_structs_are_the_structs(name):
+    cls = getattr(ssmv, name)
+    values = list(range(1, len(cls._fields_) + 1))
+    packed = cls.pack(*values)
+    assert len(packed) == ctypes.sizeof(cls)
+    assert [getattr(cls.from_buffer_copy(packed), n) for n, _ in cls._fields_] == values
