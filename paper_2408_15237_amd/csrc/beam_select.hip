@@ -284,7 +284,7 @@ __global__ __launch_bounds__(THREADS) void beam_piece_kernel(const BeamParams p)
 // ones by their places, which are in the order of row and rank.
 __global__ __launch_bounds__(1024) void beam_merge_kernel(const BeamParams p)
 {
-    constexpr int KEYS = 4;                                                       // of a lane at a time
+    constexpr int KEYS = 2;                                                       // of a lane at a time
     __shared__ __attribute__((aligned(16))) Key sLists[kMergeKeys];
     __shared__ double sScore[SSMV_BEAMS_MAX * SSMV_BEAMS_MAX];
     __shared__ int sToken[SSMV_BEAMS_MAX * SSMV_BEAMS_MAX], sDone[SSMV_BEAMS_MAX];
