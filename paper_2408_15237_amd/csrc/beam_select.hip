@@ -79,7 +79,7 @@ constexpr int kList = 1024;                                                     
 // A row may begin anywhere: its vectors are read where its own elements lie (16 bytes at the alignment of an element), so that which
 // thread takes a token, and with it the order of the sum, does not depend on the address, and equal rows stay equal to the last bit.
 // Measured: 16 x 8 rows of 128011 bf16 (33 MB) 13.5 us, of which loads and maxima alone take 6.4, the exponentials 1.7, collecting and
-// ranking 4; then 5.7 for the merge.  (All candidates ranked against all threads' best and lists merged by binary searches:
+// ranking 4; then 5.6 for the merge.  (All candidates ranked against all threads' best and lists merged by binary searches:
 // 68 us.  One workgroup for all of a sequence, in one launch: 12.7 us for one row of 32000, where two launches take 8.3.)
 template <int IO, int E>
 __global__ __launch_bounds__(THREADS) void beam_piece_kernel(const BeamParams p)
