@@ -15,6 +15,13 @@ __device__ __forceinline__ float softplus_exact(float v)
     return fmaf(__builtin_amdgcn_logf(w), 0.69314718055994531f, t - (w - 1.f)) + fmaxf(v, 0.f);
 }
 
+// A log2 e, finite: times the step 0 of a token that is none it must give 0, also where A is -inf
+__device__ __forceinline__ float decay_rate(float A)
+{
+    const float a = A * 1.4426950408889634f;
+    return a < -3.402823466e+38f ? -3.402823466e+38f : a;
+}
+
 struct CausalConvParams {
     const void *x, *wgt, *bias, *conv_in;
     const int32_t *src_row, *seq_len;

@@ -144,7 +144,6 @@ void selective_scan_kernel(const ScanParams p)
     constexpr int CH = 4, T = 64 * kHelpWaves * CH / CHW, PER_ROW = CHW / CH, U = 4;
     constexpr int BC = 2 * T * N / (64 * kHelpWaves);                             // values of B and C that a thread fetches: of one token, adjacent
     constexpr int TB = S >= 16 ? 1 : 16 / S;                                      // tokens whose B share a register
-    constexpr float LOG2E = 1.4426950408889634f;
     static_assert(S >= 1 && T % U == 0 && kScanTile % T == 0, "tile");
     __shared__ __attribute__((aligned(16))) float2 sIn[2][T][CHW];                // (dt', dt' x)
     __shared__ __attribute__((aligned(16))) float sB[2][T][N];
@@ -173,7 +172,7 @@ void selective_scan_kernel(const ScanParams p)
         float h[S], a[S];
         load_state<S>(p.A + own, a);
 #pragma unroll
-        for (int i = 0; i < S; ++i) { a[i] *= LOG2E; h[i] = 0.f; }
+        for (int i = 0; i < S; ++i) { a[i] = decay_rate(a[i]); h[i] = 0.f; }
         if (seg == 0) {
             const int src = p.src_row ? p.src_row[b] : b;
             if (OUT && p.seg_count > 1) load_state<S>(seg_h + (p.seg_count - 1) * slice + own, h);    // h_out may be h_in, and its writer another workgroup

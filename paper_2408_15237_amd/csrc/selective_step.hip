@@ -35,7 +35,6 @@ template <int IO, int N, bool DIAG, int U>
 __global__ __launch_bounds__(256) void selective_step_kernel(const TokenParams p)
 {
     constexpr int LP = N / 4, ROWS = 256 / LP;
-    constexpr float LOG2E = 1.4426950408889634f;
     const unsigned sub = threadIdx.x % LP, mine = U == 4 ? sub & 3u : 0u;
     const unsigned r_raw = blockIdx.x * ROWS + threadIdx.x / LP, total = (unsigned)p.H * p.P;
     const bool have = r_raw < total;
@@ -65,7 +64,9 @@ __global__ __launch_bounds__(256) void selective_step_kernel(const TokenParams p
         B[u].load(p.Bm, b * p.b_stride + (size_t)grp * N + 4 * sub);
         C[u].load(p.Cm, b * p.c_stride + (size_t)grp * N + 4 * sub);
     }
-    const v4 a = DIAG ? *reinterpret_cast<const v4 *>(p.A + (size_t)r * N + 4 * sub) * LOG2E : v4{1.f, 1.f, 1.f, 1.f} * (p.A[hd] * LOG2E);
+    v4 a = DIAG ? *reinterpret_cast<const v4 *>(p.A + (size_t)r * N + 4 * sub) : v4{p.A[hd], 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < (DIAG ? 4 : 1); ++i) a[i] = decay_rate(a[i]);
     const float D = p.D[hd], bias = p.dt_bias ? p.dt_bias[hd] : 0.f;
     if (p.softplus) dt = softplus_exact(dt + bias);
     const float dx = dt * x, e = DIAG ? 0.f : __builtin_amdgcn_exp2f(a[0] * dt);

@@ -177,3 +177,24 @@ def test_on_another_stream_and_in_a_graph():
         torch.cuda.synchronize()
         check_within(y, y_ref, ey, "y of a replay")
         check_within(h, h_ref, eh, "state of a replay")
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("b,n,C,N,lens", [(4, 39, 72, 16, [13, 0, 39, 38]), (2, 21, 9, 64, None), (1, 1333, 64, 32, None)])
+def test_a_decay_that_forgets_everything(io, b, n, C, N, lens):
+    """A of -inf: exp(dt' A) is 0 at every token, and tokens that fill up the last tile must still leave the state as it is."""
+    if n > 1000:
+        assert ssmv.ssm_selective_scan_workspace(b, C, N, n) > 0
+    s = _inputs(io, b, n, C, N, seed=5)
+    s["A"][:, ::3] = -float("inf")
+    s["A"][2] = -float("inf")
+    lens = None if lens is None else torch.tensor(lens, dtype=torch.int32)
+    y_ref, ey, h_ref, eh = _reference(s, io, True, None, lens)
+    assert bool(torch.isfinite(h_ref).all()) and bool(torch.isfinite(ey).all())
+    d = {k: cuda(v) for k, v in s.items()}
+    y, h = torch.zeros(b, n, C, dtype=IO[io], device="cuda"), torch.full((b, C, N), 7.0, device="cuda")
+    call(d, io, b, n, C, N, True, y, h, None, cuda(lens))
+    for i in range(b):
+        m = n if lens is None else int(lens[i])
+        check_within(y[i, :m], y_ref[i, :m], ey[i, :m], "y of sequence %d" % i)
+    check_within(h, h_ref, eh, "state")

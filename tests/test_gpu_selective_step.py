@@ -84,3 +84,23 @@ def test_steps_follow_a_prompt():
     _, ey, _, eh = scan_reference(x.cpu()[..., None], dt.cpu(), A.cpu(), B.cpu()[:, :, None], Cm.cpu()[:, :, None], D.cpu(), "f32", None, True)
     check_within(ys, y.cpu().double(), 2 * ey[..., 0], "y")
     check_within(hs, h.cpu().double(), 2 * eh[:, :, 0], "state")
+
+
+@pytest.mark.parametrize("mode,H,P,N", [("diag", 90, 1, 16), ("scalar", 6, 20, 64)])
+def test_a_decay_that_forgets_everything(mode, H, P, N):
+    """A of -inf: what a step > 0 finds is gone to the last bit, and a step of 0 leaves the state as it is."""
+    g = gen(8)
+    rows, C = 5, H * P
+    h = randn(g, rows, H, P, N).cuda()
+    A = torch.full((H, N) if mode == "diag" else (H,), -float("inf"), device="cuda")
+    dt = torch.rand(rows, H, generator=g) + 0.1
+    dt[:, ::2] = 0.0
+    x, B, Cm = randn(g, rows, C).cuda(), randn(g, rows, N).cuda(), randn(g, rows, N).cuda()
+    out = {}
+    for name, start in (("kept", h), ("empty", None)):
+        y, to = torch.empty(rows, C, device="cuda"), torch.empty_like(h)
+        ssmv.ssm_selective_step(x=x, dt=dt.cuda(), A=A, Bm=B, Cm=Cm, D=torch.zeros(H, device="cuda"), y_out=y, h_in=start, h_out=to, rows=rows, nheads=H, headdim=P,
+                                dstate=N, io="f32", a_mode=mode)
+        out[name] = to.cpu()
+    assert torch.equal(out["kept"][:, ::2], h.cpu()[:, ::2])
+    assert torch.equal(out["kept"][:, 1::2], out["empty"][:, 1::2]) and bool(torch.isfinite(out["empty"]).all())
