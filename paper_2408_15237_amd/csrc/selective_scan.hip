@@ -134,7 +134,12 @@ constexpr int kScanWaves = 4, kHelpWaves = 4;
 // registers B and C cost waits and unpacking on the scalar unit (522 us for 1 x 2048 x 8192 x 16, then in two barriers a tile, 225 with the broadcast).
 // Measured, bf16, softplus and gate, us: 16 x 2048 x 8192 x 16 909, which is 34 cycles of a SIMD for 64 values of h (24 the recurrence, 3 its LDS
 // accesses, 7 the helpers); 1 x 2048 x 8192 79 (in workgroups of 64 channels 140, those in 8 segments 106); 1 x 2048 x 1536 30 (in one
-// segment 55); 8 x 2048 x 8192 x 64 1483.
+// segment 55); 8 x 2048 x 8192 x 64 1436.
+// With 16 states a lane (N = 64 in workgroups of 64) the matrix cores add (dt' x) B, which for four channels and four state indices is a product of rank
+// one: the 4 x 4 x 1 instruction takes a column of channels, the four lanes' B, and decay h to add to - exactly the lanes' own registers, and one
+// instruction for four multiplications (8 x 2048 x 8192 x 64 1501 -> 1436, fp32 1498 -> 1456).  With eight states it made 1 % either way
+// (8 x 2048 x 8192 x 32 782 -> 773, 1 x 2048 x 8192 x 64 252 -> 255) and with four nothing (16 x 2048 x 8192 x 16 910 -> 912): every token's then
+// waits for the one before it.
 // OUT false: only the state at the segment's end and the sum of its steps, of all segments but the last.
 template <int IO, int N, int CHW, bool OUT>
 __global__ __launch_bounds__(64 * (kScanWaves + kHelpWaves)) __attribute__((amdgpu_waves_per_eu(4)))
@@ -215,11 +220,26 @@ void selective_scan_kernel(const ScanParams p)
                 unroll([&](auto uu) {
                     constexpr int u = decltype(uu)::value;
                     y[u] = 0.f;
-                    unroll([&](auto ii) {
-                        constexpr int i = decltype(ii)::value;
-                        h[i] = fmaf(h[i], __builtin_amdgcn_exp2f(a[i] * k.in[u].x), row_get<S >= 16 ? i : u % TB * S + i>(k.coef[u / TB]) * k.in[u].y);
-                        if constexpr (OUT) y[u] = fmaf(k.C[u][i], h[i], y[u]);
-                    }, std::make_integer_sequence<int, S>{});
+                    if constexpr (S >= 16) {
+                        unroll([&](auto gg) {
+                            constexpr int g = decltype(gg)::value;
+                            v4 t;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) t[i] = h[4 * g + i] * __builtin_amdgcn_exp2f(a[4 * g + i] * k.in[u].x);
+                            t = __builtin_amdgcn_mfma_f32_4x4x1f32(k.coef[u / TB], k.in[u].y, t, 2, g, 0);    // B of lanes 4g .. 4g + 3 of each 16
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                h[4 * g + i] = t[i];
+                                if constexpr (OUT) y[u] = fmaf(k.C[u][4 * g + i], t[i], y[u]);
+                            }
+                        }, std::make_integer_sequence<int, S / 4>{});
+                    } else {
+                        unroll([&](auto ii) {
+                            constexpr int i = decltype(ii)::value;
+                            h[i] = fmaf(h[i], __builtin_amdgcn_exp2f(a[i] * k.in[u].x), row_get<u % TB * S + i>(k.coef[u / TB]) * k.in[u].y);
+                            if constexpr (OUT) y[u] = fmaf(k.C[u][i], h[i], y[u]);
+                        }, std::make_integer_sequence<int, S>{});
+                    }
                     if constexpr (!OUT) sum += k.in[u].x;
                 }, std::make_integer_sequence<int, U>{});
                 if constexpr (OUT) {

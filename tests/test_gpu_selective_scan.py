@@ -198,3 +198,10 @@ def test_a_decay_that_forgets_everything(io, b, n, C, N, lens):
         m = n if lens is None else int(lens[i])
         check_within(y[i, :m], y_ref[i, :m], ey[i, :m], "y of sequence %d" % i)
     check_within(h, h_ref, eh, "state")
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [16, 32, 64])
+def test_enough_channels_to_fill_the_chip(io, N):
+    """In the widest workgroups: the last one's channels are not whole, nor are the last tokens."""
+    _run(io, 64, 11, 1000, N, lens=[11, 3, 0, 10, 1, 7, 11, 8] * 8, seed=N)
