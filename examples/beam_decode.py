@@ -43,6 +43,10 @@ class Model:
         move = lambda d: {k: v.cuda() if torch.is_tensor(v) else v for k, v in d.items() if k != "layers"}
         self.w, self.layers = move(weights), [move(x) for x in weights["layers"]]
         self.io, self.dtype = weights["io"], IO[weights["io"]]
+        self.reset()
+
+    def reset(self):
+        """Empty states: what comes next is a prompt."""
         self.h, self.conv = [None] * len(self.layers), [None] * len(self.layers)
 
     def _norm(self, x, weight):
@@ -88,6 +92,7 @@ def beam_search(model, prompts, lengths, beams, steps, eos):
     prompts [sequences][n] int32 and lengths [sequences] int32 on the GPU."""
     b, vocab = prompts.shape[0], model.w["vocab"]
     i32 = dict(dtype=torch.int32, device="cuda")
+    model.reset()
     logits = model.forward(prompts, seq_len=lengths)
     scores, done, rows_in, history = torch.zeros(b, device="cuda"), None, 1, []
     for _ in range(steps):

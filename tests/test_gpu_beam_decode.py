@@ -93,3 +93,18 @@ def test_bf16_runs():
     tokens, scores = beam_decode.beam_search(model, prompts, torch.tensor([70, 33], dtype=torch.int32, device="cuda"), 3, 6, eos=2)
     assert tokens.shape == (2, 3, 6) and bool(torch.isfinite(scores).all()) and bool((scores[:, :-1] >= scores[:, 1:]).all())
     assert int(tokens.min()) >= 0 and int(tokens.max()) < 512
+
+
+@pytest.mark.parametrize("n", [1, 40])
+def test_a_second_search_starts_from_nothing(n):
+    """One model, two searches: the second one's prompts do not go on from the first one's states."""
+    w = beam_decode.make_weights(layers=2, width=64, inner=96, dstate=16, dt_rank=6, vocab=200, io="f32", seed=3)
+    g = torch.Generator().manual_seed(6)
+    first, second = (torch.randint(3, 200, (3, m), generator=g, dtype=torch.int32).cuda() for m in (40, n))
+    lengths = torch.tensor([n, 1, (n + 1) // 2], dtype=torch.int32).cuda()
+    used = beam_decode.Model(w)
+    beam_decode.beam_search(used, first, torch.tensor([40, 3, 12], dtype=torch.int32).cuda(), 4, 5, eos=2)
+    again = beam_decode.beam_search(used, second, lengths, 4, 5, eos=2)
+    fresh = beam_decode.beam_search(beam_decode.Model(w), second, lengths, 4, 5, eos=2)
+    assert torch.equal(again[0], fresh[0])
+    assert torch.allclose(again[1], fresh[1], rtol=0, atol=2e-4)
