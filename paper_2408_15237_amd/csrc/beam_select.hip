@@ -22,25 +22,32 @@ __device__ __forceinline__ float key_logit(Key k)
 }
 __device__ __forceinline__ unsigned key_token(Key k) { return 0xffffffffu - (unsigned)k; }
 
-// v combined with the lanes 1, 2, 4, .. apart (lanes of each other half, until `size` lanes agree), without a trip through LDS
+// v combined over the wave, with the lanes 1, 2, 4, .. apart (lanes of each other half) and without a trip through LDS
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true)); }
 template <typename F>
-__device__ __forceinline__ float combine(float v, int size, F &&f)                // f(one, other, how many lanes apart)
+__device__ __forceinline__ float combine(float v, F &&f)                          // f(one, other, how many lanes apart)
 {
     v = f(v, dpp<0xB1>(v), 1);                                                    // the other lane of a pair, the other pair of a quad
     v = f(v, dpp<0x4E>(v), 2);
-    if (size >= 8) v = f(v, dpp<0x141>(v), 4);                                    // mirrored in 8, in 16
-    if (size >= 16) v = f(v, dpp<0x140>(v), 8);
-    if (size >= 32) {
-        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-        v = f(__uint_as_float(r[0]), __uint_as_float(r[1]), 16);
-    }
-    if (size >= 64) {
-        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-        v = f(__uint_as_float(r[0]), __uint_as_float(r[1]), 32);
-    }
-    return v;
+    v = f(v, dpp<0x141>(v), 4);                                                   // mirrored in 8, in 16
+    v = f(v, dpp<0x140>(v), 8);
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = f(__uint_as_float(r[0]), __uint_as_float(r[1]), 16);
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return f(__uint_as_float(r[0]), __uint_as_float(r[1]), 32);
+}
+// the largest of the lanes that are alike modulo `apart`, 1 or 2
+__device__ __forceinline__ float alike(float v, int apart)
+{
+    auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    v = fmaxf(v, dpp<0x128>(v));                                                  // 16 lanes rotated by 8, 4, 2, 1
+    v = fmaxf(v, dpp<0x124>(v));
+    v = fmaxf(v, dpp<0x122>(v));
+    return apart == 1 ? fmaxf(v, dpp<0x121>(v)) : v;
 }
 // the sum over the wave, in 64 bits
 __device__ __forceinline__ double wave_sum64(double v)
@@ -63,23 +70,35 @@ __device__ __forceinline__ double wave_sum64(double v)
     swapped([](unsigned x) { return __builtin_amdgcn_permlane32_swap(x, x, false, false); });
     return v;
 }
+__device__ __forceinline__ double lane_get(double v, int lane)
+{
+    const unsigned long long b = __builtin_bit_cast(unsigned long long, v);
+    const unsigned lo = __builtin_amdgcn_readlane((unsigned)b, lane), hi = __builtin_amdgcn_readlane((unsigned)(b >> 32), lane);
+    return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
+}
 __device__ __forceinline__ float larger(float a, float b, int) { return fmaxf(a, b); }
 __device__ __forceinline__ float sum_of(float a, float b, int) { return a + b; }
 
-constexpr int THREADS = 256, WAVES = THREADS / 64;
+constexpr int THREADS = 256, WAVES = THREADS / 64, PAIRS = THREADS / 2;
+// Up to so many candidates a bound of group maxima is as good as any; of more, the least of as many groups lets too many pass (us of a piece,
+// groups / the pairs' `keep`-th: 224 rows of 1318, 16 6.6 / 5.6, 32 14.9 / 7.1, 64 38 / 10)
+constexpr int kFewKeep = 2 * WAVES;
+// Up to so many candidates of a sequence the largest of the rows' last scores bounds the choice (us of the merge, this bound / the other one:
+// 3 rows of 6 4.9 / 5.6, 16 of 16 7.4 / 7.8, 16 of 32 10.6 / 8.2, 16 of 64 26 / 10.6)
+constexpr int kFewCandidates = 256;
 constexpr int kList = 1024;                                                       // candidates that the short way of a piece may collect
 
 // Logits are read once, and that is the least a selection can do; beside it stand a row's sum (an exponential for every logit) and
 // its best candidates.
 //
 // The best `keep` candidates of a piece of a row, best first, and its part of the row's sum; E logits of a thread at a time.
-// The threads form at least `keep` groups of equal size; the least of the groups' largest logits is a bound that at least `keep`
-// logits reach, and what reaches it is collected and ranked - some tens of candidates.  Where ties make them too many, the
+// A bound that at least `keep` logits reach: the least of the largest logits of `keep` groups of lanes, or of many the `keep`-th largest of the
+// pairs of lanes (kFewKeep).  What reaches it is collected and ranked - some tens of candidates.  Where ties make them too many, the
 // bound is taken of the threads' best keys, which are unique: only the `keep` threads at or above it can hold any candidate, keep * E at most.
 // A row may begin anywhere: its vectors are read where its own elements lie (16 bytes at the alignment of an element), so that which
 // thread takes a token, and with it the order of the sum, does not depend on the address, and equal rows stay equal to the last bit.
 // Measured: 16 x 8 rows of 128011 bf16 (33 MB) 13.5 us, of which loads and maxima alone take 6.4, the exponentials 1.7, collecting and
-// ranking 4; then 5.6 for the merge.  (All candidates ranked against all threads' best and lists merged by binary searches:
+// ranking 4; then 4.9 for the merge.  (All candidates ranked against all threads' best and lists merged by binary searches:
 // 68 us.  One workgroup for all of a sequence, in one launch: 12.7 us for one row of 32000, where two launches take 8.3.)
 template <int IO, int E>
 __global__ __launch_bounds__(THREADS) void beam_piece_kernel(const BeamParams p)
@@ -89,8 +108,8 @@ __global__ __launch_bounds__(THREADS) void beam_piece_kernel(const BeamParams p)
     constexpr float LOG2E = 1.4426950408889634f;
     __shared__ Key sList[kList + kMost];
     __shared__ Key sBest[SSMV_BEAMS_MAX], sThread[THREADS];
-    __shared__ __attribute__((aligned(16))) float sMax[SSMV_BEAMS_MAX];
-    __shared__ float sSum[WAVES];
+    __shared__ __attribute__((aligned(16))) float sMax[PAIRS];
+    __shared__ float sSum[WAVES], sLeast[2], sTop[2];
     __shared__ Key sKey;
     __shared__ int sCount;
     const unsigned tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
@@ -99,17 +118,24 @@ __global__ __launch_bounds__(THREADS) void beam_piece_kernel(const BeamParams p)
     const int done = p.done ? p.done[row] : 0;
     const char *base = static_cast<const char *>(p.logits) + row * p.row_stride * ES;
     Key *out = p.keys + (row * p.pieces + piece) * keep;
-    const int size = keep <= 4 ? 64 : keep <= 8 ? 32 : keep <= 16 ? 16 : keep <= 32 ? 8 : 4, groups = THREADS / size;
+    const int own = keep <= WAVES ? 1 : 2;                                            // groups of a wave: lanes alike modulo `own`
 
     const int begin = piece * p.piece_len, end = min(p.V, begin + p.piece_len);
     float m = -kTop, sum = 0.f, bound = -INFINITY;                                // of the chunks so far
-    // A thread's vectors of a chunk, all requested before the first is used, and a chunk ahead of its arithmetic.  One that reaches past the
+    // A thread's vectors of a chunk, all requested before the first is used, and a chunk ahead of its arithmetic.  The waves have equal
+    // shares of the chunk's vectors, a row's end too, so that no group is left with few.  A vector that reaches past the
     // end is moved back to it: the tokens ahead of its own place, which are another vector's, hold -inf then.
     uint4 raw[E / EV];
+    auto share = [&](int first) { return (min(CHUNK / EV, (end - first + EV - 1) / EV) + WAVES - 1) / WAVES; };
+    auto vector = [&](int first, int q, int i) {                                  // where the i-th begins; the end where there is none
+        const int l = i * 64 + (int)lane;
+        return l < q ? first + ((int)wave * q + l) * EV : end;
+    };
     auto fetch = [&](int first) {
+        const int q = share(first);
 #pragma unroll
         for (int i = 0; i < E / EV; ++i) {
-            const int at = min(first + i * (THREADS * EV) + (int)tid * EV, end - EV);
+            const int at = min(vector(first, q, i), end - EV);
             __builtin_memcpy(&raw[i], base + (ptrdiff_t)at * ES, sizeof(uint4));
         }
     };
@@ -130,7 +156,8 @@ __global__ __launch_bounds__(THREADS) void beam_piece_kernel(const BeamParams p)
     };
     for (int chunk = 0; chunk < p.chunks; ++chunk) {
         const int first = begin + chunk * CHUNK;
-        auto place = [&](int i) { return first + (i / EV) * (THREADS * EV) + (int)tid * EV; };
+        const int q = share(first);
+        auto place = [&](int i) { return vector(first, q, i / EV); };
         auto pos = [&](int i) { return min(place(i), end - EV) + i % EV; };
         auto there = [&](int i) { return pos(i) >= place(i); };
         float v[E];
@@ -158,15 +185,35 @@ __global__ __launch_bounds__(THREADS) void beam_piece_kernel(const BeamParams p)
         float most = -INFINITY;                                                   // (the maximum of a number and NaN is the number)
 #pragma unroll
         for (int i = 0; i < E; ++i) most = fmaxf(most, v[i]);
-        const float group = combine(most, size, larger);
-        if (tid % size == 0) sMax[tid / size] = group;
-        __syncthreads();
         const float before = m;
         float least = INFINITY;
-        for (int g = 0; g < groups; g += 4) {
-            const float4 t = *reinterpret_cast<const float4 *>(sMax + g);
-            m = fmaxf(fmaxf(fmaxf(m, t.x), fmaxf(t.y, t.z)), t.w);
-            least = fminf(fminf(least, t.x), fminf(fminf(t.y, t.z), t.w));
+        if (keep <= kFewKeep) {
+            const float group = alike(most, own);
+            if (lane < (unsigned)own) sMax[wave * own + lane] = group;
+            __syncthreads();
+            for (int g = 0; g < WAVES * own; g += 4) {
+                const float4 t = *reinterpret_cast<const float4 *>(sMax + g);
+                m = fmaxf(fmaxf(fmaxf(m, t.x), fmaxf(t.y, t.z)), t.w);
+                least = fminf(fminf(least, t.x), fminf(fminf(t.y, t.z), t.w));
+            }
+        } else {
+            const float pair = fmaxf(most, dpp<0xB1>(most));
+            if (tid % 2 == 0) sMax[tid / 2] = pair;
+            __syncthreads();
+            if (tid < PAIRS) {
+                const float mine = sMax[tid];
+                int above = 0;
+#pragma unroll 4
+                for (int g = 0; g < PAIRS; g += 4) {
+                    const float4 t = *reinterpret_cast<const float4 *>(sMax + g);
+                    above += (t.x > mine) + (t.y > mine) + (t.z > mine) + (t.w > mine);
+                }
+                const float low = combine(above < keep ? mine : INFINITY, [](float a, float b, int) { return fminf(a, b); }), top = combine(mine, larger);
+                if (lane == 0) { sLeast[wave] = low; sTop[wave] = top; }
+            }
+            __syncthreads();
+            least = fminf(sLeast[0], sLeast[1]);
+            m = fmaxf(m, fmaxf(sTop[0], sTop[1]));
         }
         if (m == INFINITY) {                                                      // +inf is the largest finite logit
             m = kTop;
@@ -180,18 +227,20 @@ __global__ __launch_bounds__(THREADS) void beam_piece_kernel(const BeamParams p)
         const bool open = bound == -INFINITY;                                     // a group without a token that is allowed
         __syncthreads();
         unsigned hits = 0;
-        int at = 0, near = 0;
-        float logit = 0.f;
+        int at = 0, near[2] = {0, 0};
+        float logit[2] = {0.f, 0.f};
         auto token = [&](unsigned bits) {                                         // of the lowest set bit
             const int i = E - 1 - __builtin_ctz(bits);
-            return min(first + i / EV * (THREADS * EV) + (int)tid * EV, end - EV) + i % EV;
+            return pos(i);
         };
         if (!open && most >= bound) {
 #pragma unroll
             for (int i = 0; i < E; ++i) hits = 2 * hits + (v[i] >= bound);
             at = atomicAdd(&sCount, __builtin_popcount(hits));
-            near = token(hits);
-            logit = load_io(base, (size_t)near, IO);                              // once more, out of the cache; back by when the sum is done
+            near[0] = token(hits);
+            near[1] = hits & (hits - 1) ? token(hits & (hits - 1)) : near[0];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) logit[k] = load_io(base, (size_t)near[k], IO);    // once more, out of the cache; back by when the sum is done
         }
         // exp(v - m) as one fused operation and exp2: the reference is what m log2 e rounds to, and the sum is corrected for that
         const bool far = fabsf(m) > 1e30f;                                        // (where the products would overflow: the difference first)
@@ -214,17 +263,18 @@ __global__ __launch_bounds__(THREADS) void beam_piece_kernel(const BeamParams p)
             part = total();
         }
         sum = fmaf(sum, __builtin_amdgcn_exp2f((before - m) * LOG2E), part);
-        while (hits && at < kList) {                                              // one, hardly ever more
-            sList[at++] = key_of(logit == INFINITY ? kTop : logit, (unsigned)near);
-            hits &= hits - 1;
-            if (hits) {
-                near = token(hits);
-                logit = load_io(base, (size_t)near, IO);
+        for (int k = 0; hits && at < kList; ++k) {                                // one, hardly ever more than two
+            if (k >= 2) {
+                near[1] = token(hits);
+                logit[1] = load_io(base, (size_t)near[1], IO);
             }
+            const float l = k == 0 ? logit[0] : logit[1];
+            sList[at++] = key_of(l == INFINITY ? kTop : l, (unsigned)(k == 0 ? near[0] : near[1]));
+            hits &= hits - 1;
         }
         const bool final = chunk + 1 == p.chunks;
         if (final) {
-            const float all = combine(sum, 64, sum_of);
+            const float all = combine(sum, sum_of);
             if (lane == 0) sSum[wave] = all;
         }
         __syncthreads();
@@ -241,9 +291,8 @@ __global__ __launch_bounds__(THREADS) void beam_piece_kernel(const BeamParams p)
             if (tid == 0) sKey = 1;                                               // every candidate there is
             __syncthreads();
             int r = 0;
-            const int used = min(THREADS, (end - first + EV - 1) / EV);           // threads that have any
 #pragma unroll 8
-            for (int i = 0; i < used; ++i) r += sThread[i] > best;
+            for (int i = 0; i < THREADS; ++i) r += sThread[i] > best;
             if (best != 0 && r == keep - 1) sKey = best;                          // keys are unique: one thread
             if (tid == 0) sCount = held;
             __syncthreads();
@@ -281,13 +330,14 @@ __global__ __launch_bounds__(THREADS) void beam_piece_kernel(const BeamParams p)
 // A workgroup per sequence.  A wave per row merges the pieces.  The largest of the lists' last logits is a bound that `keep` candidates
 // reach; so is, of at least `keep` groups of lists, the least of the groups' best.  What reaches both is moved together, and its
 // places are counted.  Then the rows of the sequence in the same way, by their scores: equal
-// ones by their places, which are in the order of row and rank.
+// ones by their places, which are in the order of row and rank; eight lanes count a place (a lane each: 16 rows of 32 16.7 us, 11.1 with eight).
 __global__ __launch_bounds__(1024) void beam_merge_kernel(const BeamParams p)
 {
     constexpr int KEYS = 2;                                                       // of a lane at a time
     __shared__ __attribute__((aligned(16))) Key sLists[kMergeKeys];
     __shared__ double sScore[SSMV_BEAMS_MAX * SSMV_BEAMS_MAX];
     __shared__ int sToken[SSMV_BEAMS_MAX * SSMV_BEAMS_MAX], sDone[SSMV_BEAMS_MAX];
+    __shared__ double sBound[7];
     __shared__ int sCount;
     const unsigned tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6, waves = blockDim.x >> 6;
     const int W = p.beams_in, keep = p.keep, pieces = p.pieces, n = pieces * keep;
@@ -325,10 +375,10 @@ __global__ __launch_bounds__(1024) void beam_merge_kernel(const BeamParams p)
             }
             continue;
         }
-        const float m = combine(part.x, 64, larger);
-        float bound = combine(worst ? key_logit(worst) : -INFINITY, 64, larger);
+        const float m = combine(part.x, larger);
+        float bound = combine(worst ? key_logit(worst) : -INFINITY, larger);
         const float best = fmaxf(first ? key_logit(first) : -INFINITY, second ? key_logit(second) : -INFINITY);
-        bound = fmaxf(bound, combine(best, 64, [&](float a, float b, int apart) { return apart * groups < 64 ? fmaxf(a, b) : fminf(a, b); }));
+        bound = fmaxf(bound, combine(best, [&](float a, float b, int apart) { return apart * groups < 64 ? fmaxf(a, b) : fminf(a, b); }));
         const double lse = log(wave_sum64((double)part.y * (double)__builtin_amdgcn_exp2f((part.x - m) * 1.4426950408889634f)));
         int count = 0;
         for (int i0 = 0; i0 < n; i0 += 64 * KEYS) {
@@ -361,24 +411,42 @@ __global__ __launch_bounds__(1024) void beam_merge_kernel(const BeamParams p)
     }
     __syncthreads();
     double bound = -INFINITY;
-    if (keep == p.beams_out)                                                      // a vocabulary of fewer tokens: all of them
-        for (int r = 0; r < W; ++r) bound = fmax(bound, sScore[r * keep + keep - 1]);
+    if (W * keep <= kFewCandidates) {
+        if (keep == p.beams_out)                                                  // a vocabulary of fewer tokens: all of them
+            for (int r = 0; r < W; ++r) bound = fmax(bound, sScore[r * keep + keep - 1]);
+    } else {
+        // j candidates of a row reach its j-th score, so `beams_out` of all rows reach the ceil(beams_out / j)-th largest of the rows' j-th
+        for (int e = wave; e < 7 && 1 << e < 2 * keep; e += waves) {
+            const int j = min(1 << e, keep), rows = (p.beams_out + j - 1) / j;
+            const double mine = (int)lane < W ? sScore[lane * keep + j - 1] : -INFINITY;
+            int above = 0;
+            for (int r = 0; r < W; ++r) above += lane_get(mine, r) > mine;
+            double low = (int)lane < W && above < rows ? mine : INFINITY;         // ties have as many above them
+            for (int apart = 1; apart < 64; apart *= 2) low = fmin(low, __shfl_xor(low, apart));
+            if (lane == 0) sBound[e] = rows <= W ? low : -INFINITY;
+        }
+        __syncthreads();
+        for (int e = 0; e < 7 && 1 << e < 2 * keep; ++e) bound = fmax(bound, sBound[e]);
+    }
     int *chosen = reinterpret_cast<int *>(sLists);                                // the lists are done with
     for (int i = tid; i < W * keep; i += blockDim.x)
         if (sScore[i] >= bound) chosen[atomicAdd(&sCount, 1)] = i;
     __syncthreads();
     const int count = sCount;
-    for (int c = tid; c < count; c += blockDim.x) {
+    for (int c = tid / 8; c < count; c += blockDim.x / 8) {                       // eight lanes to a candidate
         const int i = chosen[c], r = i / keep;
         const double s = sScore[i];
         int rank = 0;
-#pragma unroll 4
-        for (int d = 0; d < count; ++d) {
+#pragma unroll 2
+        for (int d = tid % 8; d < count; d += 8) {
             const int j = chosen[d];
             const double o = sScore[j];
             rank += o > s || (o == s && j < i);
         }
-        if (rank < p.beams_out) {
+        rank += __shfl_xor(rank, 1);
+        rank += __shfl_xor(rank, 2);
+        rank += __shfl_xor(rank, 4);
+        if (rank < p.beams_out && tid % 8 == 0) {
             const size_t at = (size_t)blockIdx.x * p.beams_out + rank, row = row0 + r;
             p.parent[at] = (int32_t)row;
             p.token[at] = sToken[i];

@@ -162,3 +162,20 @@ def test_the_same_call_gives_the_same_bits_also_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(parent.cpu().view(batch, K), first[0]) and torch.equal(token.cpu().view(batch, K), first[1]) and torch.equal(out.cpu().view(batch, K), first[2])
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [3, 10, 63, 500, 1318, 2040, 6313, 8571])
+@pytest.mark.parametrize("W,K", [(16, 9), (32, 64), (9, 33), (1, 9), (2, 3)])
+def test_ends_of_rows_and_many_candidates(io, V, W, K):
+    """Vocabularies that leave most lanes without logits; fewer tokens than beams; hundreds of candidates of a sequence, equal ones among them."""
+    K = min(K, W * V)
+    logits, scores = _inputs(3, W, V, io, V + W, masked=0.1)
+    logits[W:2 * W] = logits[W]                                   # a sequence of equal rows,
+    scores[W:2 * W] = scores[W]                                   # all of whose candidates tie
+    scores[2 * W + W // 2] = -math.inf
+    logits[2 * W, V // 2:] = -math.inf
+    _check(logits, scores, 3, K, io)
+    done = torch.zeros(3 * W, dtype=torch.int32)
+    done[::3] = 1
+    _check(logits, scores, 3, K, io, done, eos=V - 1)
