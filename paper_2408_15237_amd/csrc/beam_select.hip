@@ -379,6 +379,17 @@ __global__ __launch_bounds__(1024) void beam_merge_kernel(const BeamParams p)
         float bound = combine(worst ? key_logit(worst) : -INFINITY, larger);
         const float best = fmaxf(first ? key_logit(first) : -INFINITY, second ? key_logit(second) : -INFINITY);
         bound = fmaxf(bound, combine(best, [&](float a, float b, int apart) { return apart * groups < 64 ? fmaxf(a, b) : fminf(a, b); }));
+        if (groups > spread) {                                                    // few lists of many keys: j of a list reach its j-th, as below (48 rows of 8 lists of 32: merge 25 -> 13 us)
+            for (int j = groups / spread; j < 2 * keep; j *= 2) {
+                const int at = min(j, keep), lists = (keep + at - 1) / at;
+                if (lists > pieces) continue;
+                const Key own = (int)lane < pieces ? from[lane * keep + at - 1] : 0;
+                const float mine = own ? key_logit(own) : -INFINITY;
+                int above = 0;
+                for (int i = 0; i < pieces; ++i) above += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), i)) > mine;
+                bound = fmaxf(bound, combine((int)lane < pieces && above < lists ? mine : INFINITY, [](float a, float b, int) { return fminf(a, b); }));
+            }
+        }
         const double lse = log(wave_sum64((double)part.y * (double)__builtin_amdgcn_exp2f((part.x - m) * 1.4426950408889634f)));
         int count = 0;
         for (int i0 = 0; i0 < n; i0 += 64 * KEYS) {
