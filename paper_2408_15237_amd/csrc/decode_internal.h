@@ -38,7 +38,7 @@ struct ScanParams {
     float *h_out;
     size_t x_stride, dt_stride, b_stride, c_stride, z_stride, y_stride;
     int batch, rows_in, C, N, L, io, softplus;
-    int channels_wg;         // channels of a workgroup: 64, 32, 16 (not with N = 64)
+    int channels_wg;         // channels of a workgroup: 64, 32, 16
     int seg_len, seg_count;  // a cut prompt: tokens of a segment, segments of the longest prompt; seg_count 1: not cut
     float *seg_h;            // [batch][seg_count][C][N] end states of the segments, the first slice of each sequence; see selective_scan.hip
     float *seg_dt;           // [batch][seg_count][C]    their sums of step sizes
@@ -81,25 +81,26 @@ struct ConvHistoryParams {
 constexpr int kScanTile = 64;        // tokens of a segment: a multiple of this
 
 struct ScanPlan {
-    int channels;            // of a workgroup: 64, 32 or 16 (N < 64)
+    int channels;            // of a workgroup: 64, 32 or 16
     int seg_len, seg_count;  // tokens of a segment, segments of the longest prompt
 };
 
 // Which width of workgroup, and how many segments: the least time by a model of the kernel, whose constants were measured.  Of a
 // token a workgroup that has a compute unit to itself takes lone = 15 + N ns (16 channels), 18 + 1.6 N (32), 35 + 2.6 N (64); a compute
-// unit with k of them takes k times 14 + 0.75 N, 15 + 1.3 N, 22 + 2.5 N where that is more.  A cut prompt costs a pass over all
+// unit with k of them takes k times 14 + 0.75 N (N = 64: its LDS has room for one, k times lone), 15 + 1.3 N, 22 + 2.5 N where that is more.  A cut prompt costs a pass over all
 // segments but the last that forms their end states (0.65 of a full pass), and 5 us.
 // (us, N = 16, 2048 tokens, 64 / 32 / 16 channels: 1 x 8192 140 / 79 / 91, in 8 segments 106 / 112 / 139; 1 x 1536 137 / 78 / 55, in 16 segments
-//  36 / 30 / 37; 8 x 5120 342 / 334 / 427; 16 x 8192 909 / 1045 / 1336, in 8 segments 1481 / 1732 / 2131.  Over 20 shapes, of 1 to 32 sequences,
+//  36 / 30 / 37; 8 x 5120 342 / 334 / 427; 16 x 8192 909 / 1045 / 1336, in 8 segments 1481 / 1732 / 2131; N = 64, 32 / 16
+//  channels: 1 x 4096 x 64 64 / 45, 4 x 600 x 1024 69 / 59, 1 x 183 x 343 23 / 18.  Over 20 shapes, of 1 to 32 sequences,
 //  64 to 8192 channels and all N, its choice is within 6 % of the best of 24, noise included, but for 10 % once.)
 inline ScanPlan scan_plan(int batch, int C, int N, int L)
 {
     const int tiles = (L + kScanTile - 1) / kScanTile;
     ScanPlan best{64, L, 1};
     double least = 1e30;
-    for (int w = 64; w >= (N < 64 ? 16 : 32); w /= 2) {
+    for (int w = 64; w >= 16; w /= 2) {
         const double lone = w == 64 ? 35 + 2.6 * N : w == 32 ? 18 + 1.6 * N : 15 + 1.0 * N;
-        const double busy = w == 64 ? 22 + 2.5 * N : w == 32 ? 15 + 1.3 * N : 14 + 0.75 * N;
+        const double busy = w == 64 ? 22 + 2.5 * N : w == 32 ? 15 + 1.3 * N : N == 64 ? lone : 14 + 0.75 * N;
         const double groups = (double)batch * ((C + w - 1) / w);
         for (int want = 1; want <= 16 && want <= tiles; ++want) {
             const int len = (tiles + want - 1) / want * kScanTile, count = (L + len - 1) / len;

@@ -404,8 +404,7 @@ int launch(const ScanParams &p, hipStream_t stream)
 template <int IO, int N>
 int launch_width(const ScanParams &p, hipStream_t stream)
 {
-    if constexpr (N < 64) if (p.channels_wg == 16) return launch<IO, N, 16>(p, stream);
-    return p.channels_wg == 32 ? launch<IO, N, 32>(p, stream) : launch<IO, N, 64>(p, stream);
+    return p.channels_wg == 16 ? launch<IO, N, 16>(p, stream) : p.channels_wg == 32 ? launch<IO, N, 32>(p, stream) : launch<IO, N, 64>(p, stream);
 }
 
 template <int IO>
