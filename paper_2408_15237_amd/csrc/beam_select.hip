@@ -242,8 +242,10 @@ __global__ __launch_bounds__(THREADS) void beam_piece_kernel(const BeamParams p)
 #pragma unroll
             for (int k = 0; k < 2; ++k) logit[k] = load_io(base, (size_t)near[k], IO);    // once more, out of the cache; back by when the sum is done
         }
-        // exp(v - m) as one fused operation and exp2: the reference is what m log2 e rounds to, and the sum is corrected for that
-        const bool far = fabsf(m) > 1e30f;                                        // (where the products would overflow: the difference first)
+        // exp(v - m) as one fused operation and exp2: the reference is what m log2 e rounds to, and the sum is corrected for that.  Up to 2^20 the
+        // rounding is 2^-4 at most; of a larger m the terms would move by its powers of two (a row masked by -1e10: to 0 or infinity), so the
+        // difference comes first
+        const bool far = fabsf(m) > 1048576.f;
         const float ref = far ? 0.f : m * LOG2E;
         auto total = [&]() {
             float t = 0.f;

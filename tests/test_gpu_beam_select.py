@@ -179,3 +179,19 @@ def test_ends_of_rows_and_many_candidates(io, V, W, K):
     done = torch.zeros(3 * W, dtype=torch.int32)
     done[::3] = 1
     _check(logits, scores, 3, K, io, done, eos=V - 1)
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [500, 33001])
+@pytest.mark.parametrize("big", [3e4, 3e6, 1e9, 1e10, 1e12, 1e20, 9e29, 2e30, 1e38])
+def test_rows_at_a_large_finite_value(io, V, big):
+    """A mask that is a large finite number, in a whole row too, and logits as large: the exponentials' common reference must not cost the sum."""
+    logits, scores = _inputs(3, 2, V, io, 12)
+    logits[0:2] = -big                                            # a sequence that masks everything
+    logits[1, V - 3] = -big * 0.5
+    logits[2, ::2] = -big                                         # a row half masked beside one that is masked whole
+    logits[3] = -big
+    logits[4, ::7] = big                                          # and logits that are as large
+    logits[5, 1::9] = big
+    logits[5, 4] = big * 1.5
+    _check(logits, scores, 3, 5, io)
