@@ -143,11 +143,10 @@ inline BeamPlan beam_plan(int rows, int V, int keep)
     return r;
 }
 
-// Weak: a build of the argument checks alone (api.hip without the kernels) loads without them; its calls end on the host.
-__attribute__((weak)) int launch_causal_conv(const CausalConvParams &p, hipStream_t stream);
-__attribute__((weak)) int launch_selective_scan(const ScanParams &p, hipStream_t stream);
-__attribute__((weak)) int launch_selective_step(const TokenParams &p, hipStream_t stream);
-__attribute__((weak)) int launch_beam_select(const BeamParams &p, hipStream_t stream);
-__attribute__((weak)) int launch_conv_history(const ConvHistoryParams &p, hipStream_t stream);
+int launch_causal_conv(const CausalConvParams &p, hipStream_t stream);
+int launch_selective_scan(const ScanParams &p, hipStream_t stream);
+int launch_selective_step(const TokenParams &p, hipStream_t stream);
+int launch_beam_select(const BeamParams &p, hipStream_t stream);
+int launch_conv_history(const ConvHistoryParams &p, hipStream_t stream);
 
 }  // namespace ssmv

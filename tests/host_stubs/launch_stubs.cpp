@@ -1,6 +1,6 @@
 // Stand-ins for the kernel launchers of libssmv, for the host-only sanitizer build of the argument-validation layer
 // (csrc/api.hip): every launch "succeeds" without touching a GPU, every shape query says yes.  Test infrastructure only.
-#include "ssmv_internal.h"
+#include "decode_internal.h"
 
 namespace ssmv {
 int launch_verify_scalar(const VerifyParams &, VerifyShape, hipStream_t) { return 0; }
@@ -24,4 +24,9 @@ int launch_first_conflict(const int32_t *, const int32_t *, int, int, int32_t *,
 int launch_copy_probe(const void *, void *, void *, size_t, hipStream_t) { return 0; }
 int launch_stream_probe(int, const void *, void *, void *, size_t, int, int, hipStream_t) { return 0; }
 int launch_gated_rmsnorm(const void *, const void *, const float *, int, int, int, float, int, void *, hipStream_t) { return 0; }
+int launch_causal_conv(const CausalConvParams &, hipStream_t) { return 0; }
+int launch_selective_scan(const ScanParams &, hipStream_t) { return 0; }
+int launch_selective_step(const TokenParams &, hipStream_t) { return 0; }
+int launch_beam_select(const BeamParams &, hipStream_t) { return 0; }
+int launch_conv_history(const ConvHistoryParams &, hipStream_t) { return 0; }
 }  // namespace ssmv
