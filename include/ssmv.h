@@ -390,7 +390,7 @@ typedef struct ssmv_conv_args {
 int ssm_causal_conv(const ssmv_conv_args *args, void *hip_stream);
 
 /* A prompt through the recurrence with a decay per channel and state index (a_mode DIAG), from state to state:
- *   dt' = softplus(dt + dt_bias) (dt_softplus = 1; else dt' = dt);  h <- exp(dt' * A) * h + (dt' * x) * B_t;
+ *   dt' = softplus(dt + dt_bias) (dt_softplus = 1; else dt' = dt and dt_bias must be NULL);  h <- exp(dt' * A) * h + (dt' * x) * B_t;
  *   y = C_t . h + D * x,  y <- y * z * sigmoid(z) where z is given
  * in fp32, y rounded once to io_dtype.  x is the conv's output.  dstate in {16, 32, 64}.  An A of -inf forgets at every token
  * with dt' > 0, and at none with dt' = 0.  seq_len as above: h_out is
@@ -401,7 +401,7 @@ int ssm_causal_conv(const ssmv_conv_args *args, void *hip_stream);
 typedef struct ssmv_scan_args {
     const void *x;           /* [batch][L][channels] io_dtype                                     */
     const void *dt;          /* [batch][L][channels] io_dtype                                     */
-    const float *dt_bias;    /* [channels] fp32 or NULL                                           */
+    const float *dt_bias;    /* [channels] fp32 or NULL; only with dt_softplus                    */
     const float *A;          /* [channels][dstate] fp32, negative                                 */
     const void *Bm;          /* [batch][L][dstate] io_dtype                                       */
     const void *Cm;          /* [batch][L][dstate] io_dtype                                       */
@@ -425,7 +425,7 @@ int ssm_selective_scan_workspace(int32_t batch, int32_t channels, int32_t dstate
 typedef struct ssmv_token_args {
     const void *x;           /* [rows][H*P] io_dtype: the conv's output                           */
     const void *dt;          /* [rows][H] io_dtype                                                */
-    const float *dt_bias;    /* [H] fp32 or NULL                                                  */
+    const float *dt_bias;    /* [H] fp32 or NULL; only with dt_softplus                           */
     const float *A;          /* [H] or [H][N] fp32, negative                                      */
     const void *Bm;          /* [rows][G][N] io_dtype                                             */
     const void *Cm;          /* [rows][G][N] io_dtype                                             */

@@ -730,6 +730,7 @@ int ssm_selective_scan(const ssmv_scan_args *args, void *hip_stream)
     TRY(check_io(a.y_out, a.io_dtype, "y_out"));
     if (a.z) TRY(check_io(a.z, a.io_dtype, "z"));
     if (a.dt_bias) TRY(check_f32(a.dt_bias, "dt_bias"));
+    if (a.dt_bias && !a.dt_softplus) return fail(SSMV_EINVAL, "dt_bias is added inside the softplus: without dt_softplus it must be NULL");
     if (a.h_in) TRY(check_ptr(a.h_in, "h_in"));
     if (a.h_out) TRY(check_ptr(a.h_out, "h_out"));
     if (!aligned_to(a.seq_len, 4)) return fail(SSMV_EALIGN, "seq_len is not 4-byte aligned");
@@ -788,6 +789,7 @@ int ssm_selective_step(const ssmv_token_args *args, void *hip_stream)
     if (a.h_in) TRY(check_ptr(a.h_in, "h_in"));
     if (a.z) TRY(check_io(a.z, a.io_dtype, "z"));
     if (a.dt_bias) TRY(check_f32(a.dt_bias, "dt_bias"));
+    if (a.dt_bias && !a.dt_softplus) return fail(SSMV_EINVAL, "dt_bias is added inside the softplus: without dt_softplus it must be NULL");
     if (a.src_row && a.h_out == a.h_in) return fail(SSMV_EINVAL, "h_out may be h_in only without src_row");
     TokenParams p{};
     p.x = a.x; p.dt = a.dt; p.Bm = a.Bm; p.Cm = a.Cm; p.z = a.z; p.dt_bias = a.dt_bias; p.A = a.A; p.D = a.D; p.h_in = a.h_in; p.src_row = a.src_row;

@@ -117,3 +117,11 @@ def test_packed_structs_are_the_structs(name):
     packed = cls.pack(*values)
     assert len(packed) == ctypes.sizeof(cls)
     assert [getattr(cls.from_buffer_copy(packed), n) for n, _ in cls._fields_] == values
+
+
+@pytest.mark.parametrize("fn,args", [("ssm_selective_scan", SCAN), ("ssm_selective_step", STEP)])
+def test_a_bias_without_softplus_is_refused(fn, args):
+    """The step without softplus is taken as given; a bias that would not be added is an error, not a silence."""
+    with pytest.raises(ssmv.SsmvError, match="dt_bias") as ei:
+        getattr(ssmv, fn)(**{**args, "dt_bias": P, "dt_softplus": False, "h_in": P, "h_out": P, "src_row": P})   # (which would end the call later)
+    assert ei.value.code == ssmv.SSMV_EINVAL
