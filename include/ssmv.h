@@ -392,8 +392,8 @@ int ssm_causal_conv(const ssmv_conv_args *args, void *hip_stream);
 /* A prompt through the recurrence with a decay per channel and state index (a_mode DIAG), from state to state:
  *   dt' = softplus(dt + dt_bias) (dt_softplus = 1; else dt' = dt and dt_bias must be NULL);  h <- exp(dt' * A) * h + (dt' * x) * B_t;
  *   y = C_t . h + D * x,  y <- y * z * sigmoid(z) where z is given
- * in fp32, y rounded once to io_dtype.  x is the conv's output.  dstate in {16, 32, 64}.  An A of -inf forgets at every token
- * with dt' > 0, and at none with dt' = 0.  seq_len as above: h_out is
+ * in fp32, y rounded once to io_dtype.  x is the conv's output.  dstate in {16, 32, 64}.  An A of -inf (it counts as the
+ * lowest finite fp32 / log2 e) forgets at every token with dt' >= 2^-120, and at none with dt' = 0.  seq_len as above: h_out is
  * the state after a sequence's own tokens.
  * Few sequences and channels and a long prompt: the prompt is cut into segments that run side by side; their end states need
  * `workspace` (ssm_selective_scan_workspace bytes, 0 where nothing is cut; SSMV_EINVAL where it is needed and NULL).  The cut depends on

@@ -15,7 +15,8 @@ __device__ __forceinline__ float softplus_exact(float v)
     return fmaf(__builtin_amdgcn_logf(w), 0.69314718055994531f, t - (w - 1.f)) + fmaxf(v, 0.f);
 }
 
-// A log2 e, finite: times the step 0 of a token that is none it must give 0, also where A is -inf
+// A log2 e, finite: times the step 0 of a token that is none it must give 0, also where A is -inf.  (Steps below 2^-121 then leave
+// something of the state: exp2 of the lowest finite value times so little is not 0.)
 __device__ __forceinline__ float decay_rate(float A)
 {
     const float a = A * 1.4426950408889634f;

@@ -205,3 +205,23 @@ def test_a_decay_that_forgets_everything(io, b, n, C, N, lens):
 def test_enough_channels_to_fill_the_chip(io, N):
     """In the widest workgroups: the last one's channels are not whole, nor are the last tokens."""
     _run(io, 64, 11, 1000, N, lens=[11, 3, 0, 10, 1, 7, 11, 8] * 8, seed=N)
+
+
+@pytest.mark.parametrize("C,N", [(72, 16), (5, 32), (70, 64)])
+def test_the_least_step_that_forgets(C, N):
+    """A of -inf and steps of 2^-120: nothing of the start is left, to the last bit; after a step of 0 all of it."""
+    b, n = 2, 21
+    s = _inputs("f32", b, n, C, N, soft=False, gate=False, seed=6)
+    s["A"][:] = -float("inf")
+    for step, forgets in ((2.0 ** -120, True), (0.0, False)):
+        s["dt"][:] = step
+        out = []
+        for start in (s["h_in"], torch.zeros_like(s["h_in"])):
+            d = {k: cuda(v) for k, v in dict(s, h_in=start).items()}
+            y, h = torch.zeros(b, n, C, device="cuda"), torch.full((b, C, N), 7.0, device="cuda")
+            call(d, "f32", b, n, C, N, False, y, h)
+            out.append((y.cpu(), h.cpu()))
+        if forgets:
+            assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
+        else:
+            assert torch.equal(out[0][1], s["h_in"])

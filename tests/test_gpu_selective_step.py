@@ -104,3 +104,20 @@ def test_a_decay_that_forgets_everything(mode, H, P, N):
         out[name] = to.cpu()
     assert torch.equal(out["kept"][:, ::2], h.cpu()[:, ::2])
     assert torch.equal(out["kept"][:, 1::2], out["empty"][:, 1::2]) and bool(torch.isfinite(out["empty"]).all())
+
+
+@pytest.mark.parametrize("mode,H,P,N", [("diag", 90, 1, 16), ("scalar", 6, 20, 64)])
+def test_the_least_step_that_forgets(mode, H, P, N):
+    """A of -inf and a step of 2^-120: nothing of the start is left, to the last bit."""
+    g = gen(9)
+    rows, C = 5, H * P
+    h = randn(g, rows, H, P, N).cuda()
+    A = torch.full((H, N) if mode == "diag" else (H,), -float("inf"), device="cuda")
+    x, B, Cm = randn(g, rows, C).cuda(), randn(g, rows, N).cuda(), randn(g, rows, N).cuda()
+    out = []
+    for start in (h, None):
+        y, to = torch.empty(rows, C, device="cuda"), torch.empty_like(h)
+        ssmv.ssm_selective_step(x=x, dt=torch.full((rows, H), 2.0 ** -120, device="cuda"), A=A, Bm=B, Cm=Cm, D=torch.zeros(H, device="cuda"), y_out=y, h_in=start, h_out=to,
+                                rows=rows, nheads=H, headdim=P, dstate=N, io="f32", a_mode=mode)
+        out.append((y.cpu(), to.cpu()))
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
