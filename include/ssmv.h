@@ -441,8 +441,11 @@ typedef struct ssmv_token_args {
 int ssm_selective_step(const ssmv_token_args *args, void *hip_stream);
 
 /* Beam search's choice: of the candidates (row r, token v) of every sequence's beams_in rows, with the score
- *   scores[r] + logits[r][v] - logsumexp(logits[r])     (differences and sums of candidates in 64 bits),
+ *   scores[r] + logits[r][v] - logsumexp(logits[r]),
  * the beams_out best, best first; equal scores by the lower row, inside a row by the higher logit, then the lower token.
+ * Differences, logarithms and sums of candidates are taken in 64 bits, a row's sum of exponentials in 32: logsumexp is off by about 1e-7, by
+ * less than 3e-6 always, and candidates of different rows that are nearer than that may change places.  Inside a row the order is that of the logits;
+ * rows that are equal have equal sums, so that their candidates tie.
  * parent holds rows of the whole batch (sequence * beams_in + beam), ready to be the src_row of the next step's calls.
  *   - done (device int32 [batch*beams_in], or NULL): a row with done != 0 is a finished hypothesis: its logits do not count, its
  *     one candidate is itself, token `eos` with its score unchanged (further places of it: eos with score -inf).  done_out
