@@ -97,9 +97,10 @@ constexpr int kList = 1024;                                                     
 // bound is taken of the threads' best keys, which are unique: only the `keep` threads at or above it can hold any candidate, keep * E at most.
 // A row may begin anywhere: its vectors are read where its own elements lie (16 bytes at the alignment of an element), so that which
 // thread takes a token, and with it the order of the sum, does not depend on the address, and equal rows stay equal to the last bit.
-// Measured: 16 x 8 rows of 128011 bf16 (33 MB) 13.5 us, of which loads and maxima alone take 6.4, the exponentials 1.7, collecting and
-// ranking 4; then 4.9 for the merge.  (All candidates ranked against all threads' best and lists merged by binary searches:
-// 68 us.  One workgroup for all of a sequence, in one launch: 12.7 us for one row of 32000, where two launches take 8.3.)
+// Measured: 16 x 8 rows of 128011 bf16 (33 MB) 13.7 us, of which loads and maxima alone take 6.4, the exponentials 1.7, collecting and
+// ranking 4 (vector instructions 6.0 in all, waits half of the waves' time); then 4.9 for the merge.  128 x 8 rows 72 us,
+// 3.6 TB/s, vector instructions 43.  (All candidates ranked against all threads' best and lists merged by binary searches: 68 us.  One workgroup for
+// all of a sequence, in one launch: 12.7 us for one row of 32000, where two launches take 8.3.)
 template <int IO, int E>
 __global__ __launch_bounds__(THREADS) void beam_piece_kernel(const BeamParams p)
 {

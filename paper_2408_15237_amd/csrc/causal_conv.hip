@@ -56,11 +56,13 @@ struct Chunk {
     }
 };
 
-// Bound by memory: a token row in, a token row out (8 x 2048 x 5120 bf16, 336 MB, other tensors in every call: 60.8 us, 5.5 TB/s; copies of 1 GB 5.1 to 6.1).
+// Bound by memory: a token row in, a token row out (8 x 2048 x 5120 bf16, 336 MB, other tensors in every call: 60.5 to 62.6 us, 5.4 to 5.5 TB/s; copies of 1 GB 5.1 to 6.1).
 // A thread owns VEC adjacent channels of T tokens: it requests its tokens and the three before them together, and slides over
-// them in registers.  The three are those of the thread of the tokens before, 2^lanes threads ahead in the same workgroup but for one
-// tile in 256 / 2^lanes, so that they come out of the L1 and what a workgroup reads does not depend on where others run.  The first tokens
-// take the history, and their thread also leaves the newest three inputs, so that conv_out may be conv_in.
+// them in registers.  The three are those of the thread of the tokens before, 2^lanes threads ahead in the same workgroup, and come out of the
+// L1 - but for the workgroup's first tile, one in 256 / 2^lanes: with 64 vectors side by side one in four, so that 19 tokens are read from beyond
+// it for 16 written (8 x 2048 x 5120 bf16: FETCH_SIZE x 2 = 1.19 WRITE_SIZE).  What a workgroup reads does not depend on where others run.  The first tokens
+// take the history, and their thread also leaves the newest three inputs, so that conv_out may be conv_in.  (The choice of a history vector by the
+// sequence's length, at the end, keeps the three in 64 bytes of scratch memory a lane.)
 template <int IO, int VEC, int T, bool PAST>
 __global__ __launch_bounds__(256) void causal_conv_kernel(const CausalConvParams p, int lanes, unsigned chunks, unsigned groups)
 {

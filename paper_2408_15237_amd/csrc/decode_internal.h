@@ -92,8 +92,8 @@ struct ScanPlan {
 // segments but the last that forms their end states (0.65 of a full pass), and 5 us.
 // (us, N = 16, 2048 tokens, 64 / 32 / 16 channels: 1 x 8192 140 / 79 / 91, in 8 segments 106 / 112 / 139; 1 x 1536 137 / 78 / 55, in 16 segments
 //  36 / 30 / 37; 8 x 5120 342 / 334 / 427; 16 x 8192 909 / 1045 / 1336, in 8 segments 1481 / 1732 / 2131; N = 64, 32 / 16
-//  channels: 1 x 4096 x 64 64 / 45, 4 x 600 x 1024 69 / 59, 1 x 183 x 343 23 / 18.  Over 20 shapes, of 1 to 32 sequences,
-//  64 to 8192 channels and all N, its choice is within 6 % of the best of 24, noise included, but for 10 % once.)
+//  channels: 1 x 4096 x 64 64 / 45, 4 x 600 x 1024 69 / 59, 1 x 183 x 343 23 / 18.  Over 29 shapes, of 1 to 32 sequences, 64 to
+//  8192 channels and all N, its choice is the best of up to 24 in 23, and 1 to 6 % slower than the best in the others.)
 inline ScanPlan scan_plan(int batch, int C, int N, int L)
 {
     const int tiles = (L + kScanTile - 1) / kScanTile;
@@ -130,7 +130,7 @@ struct BeamPlan {
 };
 
 // Small chunks where large ones would be too few to fill the chip, and few candidates are kept of each.  Of large ones a piece takes
-// several where that leaves four workgroups for every compute unit.
+// several where that leaves 1024 workgroups: as many as run at once with bf16 logits (four on a compute unit; of fp32 ones, with 131 registers, three).
 inline BeamPlan beam_plan(int rows, int V, int keep)
 {
     BeamPlan r;

@@ -133,8 +133,8 @@ constexpr int kScanWaves = 4, kHelpWaves = 4;
 // B of a token is a broadcast operand of the multiplication (16 / S tokens' worth sit in the lanes of every 16 of a register); as scalar
 // registers B and C cost waits and unpacking on the scalar unit (522 us for 1 x 2048 x 8192 x 16, then in two barriers a tile, 225 with the broadcast).
 // Measured, bf16, softplus and gate, us: 16 x 2048 x 8192 x 16 909, which is 34 cycles of a SIMD for 64 values of h (24 the recurrence, 3 its LDS
-// accesses, 7 the helpers); 1 x 2048 x 8192 79 (in workgroups of 64 channels 140, those in 8 segments 106); 1 x 2048 x 1536 30 (in one
-// segment 55); 8 x 2048 x 8192 x 64 1436.
+// accesses, 7 the helpers); 1 x 2048 x 8192 80 with the same inputs in every call, out of the caches (in workgroups of 64 channels 140, those in 8 segments
+// 107), 85 with others, out of memory; 1 x 2048 x 1536 30 to 32 (in one segment 55); 8 x 2048 x 8192 x 64 1436.
 // With 16 states a lane (N = 64 in workgroups of 64) the matrix cores add (dt' x) B, which for four channels and four state indices is a product of rank
 // one: the 4 x 4 x 1 instruction takes a column of channels, the four lanes' B, and decay h to add to - exactly the lanes' own registers, and one
 // instruction for four multiplications (8 x 2048 x 8192 x 64 1501 -> 1436, fp32 1498 -> 1456).  With eight states it made 1 % either way
