@@ -5,15 +5,16 @@
 #include <cstdio>
 #include <cstring>
 
+#include "api_checks.h"
 #include "decode_internal.h"
 
 using namespace ssmv;
 
 namespace {
-
 thread_local char g_err[512] = "";
+}
 
-int fail(int code, const char *fmt, ...)
+int ssmv::fail(int code, const char *fmt, ...)
 {
     va_list ap;
     va_start(ap, fmt);
@@ -22,17 +23,17 @@ int fail(int code, const char *fmt, ...)
     return code;
 }
 
-int hip_fail(int hip_code, const char *what)
+int ssmv::hip_fail(int hip_code, const char *what)
 {
     return fail(SSMV_EHIP, "%s: %s", what, hipGetErrorString((hipError_t)hip_code));
 }
+
+namespace {
 
 std::atomic<int> g_tune_rows{0};
 std::atomic<int> g_tune_waves{0};
 
 bool is_pow2(int v) { return v > 0 && (v & (v - 1)) == 0; }
-size_t io_bytes(int io) { return io == SSMV_BF16 ? 2 : 4; }
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 int check_dims(const ssmv_dims *d)
 {
@@ -95,13 +96,6 @@ bool state_tiled(const ssmv_dims *d)
 {
     return d->engine == SSMV_ENGINE_AUTO && d->a_mode == SSMV_A_SCALAR && d->io_dtype == SSMV_BF16 &&
            verify_mfma_supported(d->dstate, d->headdim) && pend_max_of(d) + d->kmax <= 16;
-}
-
-int check_ptr(const void *p, const char *name)
-{
-    if (!p) return fail(SSMV_EINVAL, "%s is NULL", name);
-    if (!aligned16(p)) return fail(SSMV_EALIGN, "%s (%p) is not 16-byte aligned", name, p);
-    return SSMV_OK;
 }
 
 int check_cache(const ssmv_cache *c)
@@ -598,52 +592,6 @@ int ssmv_copy_probe(const void *src, void *dst0, void *dst1, size_t n_bytes, voi
 }  // extern "C"
 
 // ---- plain and beam decoding ---------------------------------------------------------------------------------------------
-
-namespace {
-
-bool aligned_to(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
-
-// a tensor of the I/O type that needs only its elements' alignment
-int check_io(const void *p, int io, const char *name)
-{
-    if (!p) return fail(SSMV_EINVAL, "%s is NULL", name);
-    if (!aligned_to(p, io_bytes(io))) return fail(SSMV_EALIGN, "%s (%p) is not aligned to its elements", name, p);
-    return SSMV_OK;
-}
-
-int check_f32(const void *p, const char *name)
-{
-    if (!p) return fail(SSMV_EINVAL, "%s is NULL", name);
-    if (!aligned_to(p, 4)) return fail(SSMV_EALIGN, "%s (%p) is not 4-byte aligned", name, p);
-    return SSMV_OK;
-}
-
-// 0 = packed
-int check_stride(int64_t *stride, long packed, const char *name)
-{
-    if (*stride == 0) *stride = packed;
-    if (*stride < packed || *stride > (int64_t)1 << 40)
-        return fail(SSMV_EINVAL, "%s %lld: rows of %ld elements would overlap, or it is beyond 2^40", name, (long long)*stride, packed);
-    return SSMV_OK;
-}
-
-int check_io_type(int io)
-{
-    return io == SSMV_F32 || io == SSMV_BF16 ? SSMV_OK : fail(SSMV_EINVAL, "io_dtype %d unknown", io);
-}
-
-int check_rows(int32_t *rows_in, int rows, const int32_t *src_row)
-{
-    if (*rows_in == 0) *rows_in = rows;
-    if (*rows_in < 0) return fail(SSMV_EINVAL, "rows_in %d < 0", *rows_in);
-    if (!src_row && *rows_in < rows) return fail(SSMV_EINVAL, "rows_in %d < %d rows that go out, and no src_row", *rows_in, rows);
-    if (!aligned_to(src_row, 4)) return fail(SSMV_EALIGN, "src_row is not 4-byte aligned");
-    return SSMV_OK;
-}
-
-#define TRY(call) do { const int rc_ = (call); if (rc_ != SSMV_OK) return rc_; } while (0)
-
-}  // namespace
 
 extern "C" {
 
