@@ -54,11 +54,11 @@ class ssmv_prefill_args(ctypes.Structure):
         (n, ctypes.c_int32) for n in ("L", "dt_softplus")]
 
 
-def _args_struct(name, pointers, longs, ints):
+def _args_struct(name, pointers, longs, ints, floats=()):
     """The ctypes form of an argument struct; `pack` makes its bytes from the fields' values in half the time."""
     cls = type(name, (ctypes.Structure,), {"_fields_": [(n, ctypes.c_void_p) for n in pointers] + [(n, ctypes.c_int64) for n in longs] +
-                                           [(n, ctypes.c_int32) for n in ints]})
-    cls.pack = struct.Struct("%dP%dq%di0P" % (len(pointers), len(longs), len(ints))).pack        # 0P: padded like the C struct
+                                           [(n, ctypes.c_int32) for n in ints] + [(n, ctypes.c_float) for n in floats]})
+    cls.pack = struct.Struct("%dP%dq%di%df0P" % (len(pointers), len(longs), len(ints), len(floats))).pack        # 0P: padded like the C struct
     return cls
 
 

@@ -1,0 +1,211 @@
+// Parameter blocks, launchers and common device code of the layer operators (block_norm.hip, gated_recurrence.hip, gated_backward.hip,
+// logit_rules.hip).
+#pragma once
+
+#include "ssmv_internal.h"
+#include "ssmv_layers.h"
+
+namespace ssmv {
+
+struct BlockNormParams {
+    const void *x, *z, *res;
+    const float *post, *scale, *pre;
+    void *r_out, *n_out;
+    size_t x_stride, z_stride, res_stride, r_stride, n_stride;
+    int rows, C, io, res_io;
+    float eps, alpha;
+};
+
+struct BlockNormGradParams {
+    const void *x, *z, *res;
+    const float *post, *scale, *pre;
+    const void *dr, *dn;
+    void *dx, *dz, *dres;
+    float *dpost, *dscale, *dpre;
+    float *partial;          // [parts][3][C]: dpre, dscale, dpost of a workgroup's rows; NULL: none is wanted
+    size_t x_stride, z_stride, res_stride, dr_stride, dn_stride, dx_stride, dz_stride, dres_stride;
+    int rows, C, io, res_io, parts;
+    float eps, alpha;
+};
+
+struct GatedParams {
+    const void *x, *f, *i, *z;
+    const float *A, *f_bias, *i_bias, *h_in;
+    const int32_t *src_row, *seq_len;
+    void *y;
+    float *h_out, *states;
+    size_t x_stride, f_stride, i_stride, z_stride, y_stride;
+    int batch, rows_in, C, L, io, lru;
+    int lanes;               // channel lanes of a wave: see GatedPlan
+    int seg_len, seg_count;
+    float *seg_p;            // [batch][seg_count][C] products of the segments' decays
+    float *seg_h;            // [batch][seg_count][C] end states of the segments from zero (the first one's from its start); last place: the start state
+};
+
+struct GatedGradParams {
+    const void *x, *f, *i, *z, *dy;
+    const float *A, *f_bias, *i_bias, *states, *dh_out;
+    const int32_t *seq_len;
+    void *dx, *df, *di, *dz;
+    float *dA, *df_bias, *di_bias, *dh_in;
+    size_t x_stride, f_stride, i_stride, z_stride, dy_stride, dx_stride, df_stride, di_stride, dz_stride;
+    int batch, C, L, io, lru;
+    int lanes, seg_len, seg_count;
+    float *seg_p;            // [batch][seg_count][C] products of the segments' decays
+    float *seg_r;            // [batch][seg_count][C] what flows out of a segment's front when nothing flows into its end
+    float *partial;          // [batch][seg_count][3][C] sums for A, f_bias, i_bias of a segment's tokens; NULL: none is wanted
+};
+
+struct RulesParams {
+    const void *logits;
+    const int32_t *hist, *hist_len, *src_row, *token, *prompt_len;
+    const float *repetition, *frequency, *presence;
+    const int32_t *bias_token;
+    const float *bias;
+    const uint32_t *mask;
+    const int32_t *mask_row;
+    void *out;
+    int32_t *hist_out, *hist_len_out;
+    size_t row_stride, out_stride, mask_stride;
+    int rows, rows_in, V, io, room, bias_n, mask_rows;
+};
+
+int launch_block_norm(const BlockNormParams &p, hipStream_t stream);
+int launch_block_norm_backward(const BlockNormGradParams &p, hipStream_t stream);
+int launch_gated_recurrence(const GatedParams &p, hipStream_t stream);
+int launch_gated_backward(const GatedGradParams &p, hipStream_t stream);
+int launch_logit_rules(const RulesParams &p, hipStream_t stream);
+
+// Sums over the rows of partial [parts][n_out][C]: out[k][c], divided by over[c] where that is given (0 where over[c] is 0).
+struct ColumnSums {
+    float *out[3];
+    const float *over[3];
+};
+int launch_column_sums(const float *partial, int parts, int C, const ColumnSums &to, hipStream_t stream);
+
+// Rows' weight gradients are summed by so many workgroups (threads of a row: see norm_threads).
+constexpr int kNormParts = 512;
+inline int norm_parts(int rows) { return rows < kNormParts ? (rows + 3) / 4 * 4 : kNormParts; }     // a workgroup holds up to four rows
+
+// How the recurrence is laid on the chip.  A workgroup takes 512 threads; `lanes` lanes of a wave lie side by side over the channels (two bf16
+// channels a lane, or one fp32), the others over the tokens, 8 a lane: 64 * 64 / lanes tokens a tile.
+struct GatedPlan {
+    int lanes;               // 64, 32, 16, 8
+    int seg_len, seg_count;  // tokens of a segment (whole tiles), segments of the longest sequence
+};
+inline GatedPlan gated_plan(int batch, int C, int L)
+{
+    // counted in fp32 lanes, so that the plan, and with it the workspace, does not depend on the type
+    GatedPlan r{64, L, 1};
+    auto groups = [&](int lanes) { return (long)batch * ((C + lanes - 1) / lanes); };
+    while (r.lanes > 8 && groups(r.lanes) < 512 && L > 4096 / r.lanes) r.lanes /= 2;
+    const int tile = 4096 / r.lanes, tiles = (L + tile - 1) / tile;
+    int want = 1;
+    while (want < 16 && groups(r.lanes) * want < 256 && tiles >= 8 * want) want *= 2;
+    if (want > 1) {
+        r.seg_len = (tiles + want - 1) / want * tile;
+        r.seg_count = (L + r.seg_len - 1) / r.seg_len;
+        if (r.seg_count == 1) r.seg_len = L;
+    }
+    return r;
+}
+
+// ---- device code --------------------------------------------------------------------------------------------------------
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
+
+// 8 adjacent elements at any alignment, `live` of them: the others are not touched and count as 0
+template <int T>
+__device__ __forceinline__ void load8(const void *base, size_t idx, int live, float (&v)[8])
+{
+    if (live == 8) {
+        if constexpr (T == SSMV_BF16) {
+            uint4 r;
+            __builtin_memcpy(&r, static_cast<const char *>(base) + idx * 2, sizeof(r));
+            IoVec<SSMV_BF16>::decode(r, v);
+        } else {
+            __builtin_memcpy(v, static_cast<const char *>(base) + idx * 4, sizeof(v));
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = j < live ? load_io(base, idx + j, T) : 0.f;
+    }
+}
+
+template <int T>
+__device__ __forceinline__ void store8(void *base, size_t idx, int live, const float (&v)[8])
+{
+    if (live == 8) {
+        if constexpr (T == SSMV_BF16) {
+            const uint4 r = IoVec<SSMV_BF16>::encode(v);
+            __builtin_memcpy(static_cast<char *>(base) + idx * 2, &r, sizeof(r));
+        } else {
+            __builtin_memcpy(static_cast<char *>(base) + idx * 4, v, sizeof(v));
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < live) store_io(base, idx + j, v[j], T);
+    }
+}
+
+// sigmoid(v) and 1 - sigmoid(v), both to within a few roundings for every v
+__device__ __forceinline__ void sigmoids(float v, float &s, float &other)
+{
+    const float t = __builtin_amdgcn_exp2f(-kLog2e * fabsf(v)), w = __builtin_amdgcn_rcpf(1.f + t), tw = t * w;
+    s = v < 0.f ? tw : w;
+    other = v < 0.f ? w : tw;
+}
+__device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * v)); }
+
+// A log2 e, finite (a decay of 0 must stay 0 times anything)
+__device__ __forceinline__ float decay_exponent(float A)
+{
+    const float a = A * kLog2e;
+    return a < -3.402823466e+38f ? -3.402823466e+38f : a;
+}
+
+// 1 - a^2 for a = 2^q, q <= 0: near a = 1, where the difference loses it, -expm1(u) at u = 2 q ln 2 by its series
+// -u (1 + u/2 + u^2/6 + ... + u^6/5040), off by less than 2e-8 for |u| < 0.35; elsewhere a^2 is at most 0.71 and its roundings count 2.4 times.
+__device__ __forceinline__ float one_minus_square(float q, float a)
+{
+    const float u = 2.f * kLn2 * q;
+    float s = fmaf(u, 1.f / 5040, 1.f / 720);
+    s = fmaf(s, u, 1.f / 120);
+    s = fmaf(s, u, 1.f / 24);
+    s = fmaf(s, u, 1.f / 6);
+    s = fmaf(s, u, 0.5f);
+    s = fmaf(s, u, 1.f);
+    return u > -0.35f ? -u * s : fmaf(-a, a, 1.f);
+}
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float add_dpp(float v)
+{
+    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, ROWS, 0xf, false));
+}
+// the sum over a wave, in every lane
+__device__ __forceinline__ float sum_of_wave(float v)
+{
+    v = add_dpp<0x111, 0xf>(v);     // row_shr:1, 2, 4, 8: lane 15 of a row holds the row's sum
+    v = add_dpp<0x112, 0xf>(v);
+    v = add_dpp<0x114, 0xf>(v);
+    v = add_dpp<0x118, 0xf>(v);
+    v = add_dpp<0x142, 0xa>(v);     // row_bcast:15 into rows 1 and 3
+    v = add_dpp<0x143, 0xc>(v);     // row_bcast:31 into rows 2 and 3
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
+// The z-th longest of up to 64 sequences: workgroups start in the order of their indexes, and a long sequence that starts last has the chip to itself.
+__device__ __forceinline__ int zth_longest(const int32_t *seq_len, int batch, int z, unsigned lane)
+{
+    const int mine = (int)lane < batch ? seq_len[lane] : 0;
+    int rank = 0;
+    for (int i = 0; i < batch; ++i) {
+        const int other = __builtin_amdgcn_readlane(mine, i);
+        rank += other > mine || (other == mine && i < (int)lane);
+    }
+    return __builtin_ctzll(__ballot((int)lane < batch && rank == z));
+}
+
+}  // namespace ssmv
