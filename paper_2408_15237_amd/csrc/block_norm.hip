@@ -26,9 +26,77 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*part)[kMaxWaves]
     }
 }
 
+// 8 adjacent channels of a row as stored.  The last ones of a row are a vector moved back, whose first `skip` channels are another thread's: they count as zeros here and
+// are not stored.  Threads behind the row have skip 8.  A row of fewer than 8 channels is loaded by elements (SMALL).
+template <int T>
+struct Eight {
+    uint4 w[T == SSMV_BF16 ? 1 : 2];
+    template <bool SMALL>
+    __device__ __forceinline__ void load(const void *base, size_t idx, int C)
+    {
+        constexpr int ES = T == SSMV_BF16 ? 2 : 4;
+        if constexpr (!SMALL) {
+            __builtin_memcpy(w, static_cast<const char *>(base) + idx * ES, sizeof(w));
+        } else {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = j < C ? load_io(base, idx + j, T) : 0.f;
+            if constexpr (T == SSMV_BF16) w[0] = IoVec<T>::encode(v);
+            else __builtin_memcpy(w, v, sizeof(w));
+        }
+    }
+    __device__ __forceinline__ void get(float (&v)[8], int skip) const
+    {
+        if constexpr (T == SSMV_BF16) IoVec<T>::decode(w[0], v);
+        else __builtin_memcpy(v, w, sizeof(w));
+        if (skip != 0) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = j < skip ? 0.f : v[j];
+        }
+    }
+};
+
+template <int T, bool SMALL>
+__device__ __forceinline__ void put(void *base, size_t idx, int skip, int C, const float (&v)[8])
+{
+    if (!SMALL && skip == 0) {
+        store8<T>(base, idx, 8, v);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j >= skip && (!SMALL || j < C)) store_io(base, idx + j, v[j], T);
+    }
+}
+
+template <bool SMALL>
+__device__ __forceinline__ void weights(const float *from, int c0, int C, float (&w)[8])
+{
+    if constexpr (!SMALL) {
+        __builtin_memcpy(w, from + c0, sizeof(w));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = j < C ? from[c0 + j] : 0.f;
+    }
+}
+
+// where a thread's channels are
+template <int NV, bool SMALL>
+struct Place {
+    int c0[NV], skip[NV];
+    __device__ __forceinline__ Place(int t, int threads, int C)
+    {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int own = (t + k * threads) * 8;
+            c0[k] = SMALL ? 0 : min(own, C - 8);
+            skip[k] = SMALL ? (own == 0 ? 0 : 8) : min(own - c0[k], 8);
+        }
+    }
+};
+
 // Bound by memory: x, z and res in, r and n out.  `waves` waves to a row, as many rows as the workgroup has room for; a thread owns NV times 8 adjacent
-// channels of its row, which stay in registers between the passes.
-template <int IO, int RES, int NV>
+// channels of its row, which stay in registers between the passes.  Everything is requested before the first wait.
+template <int IO, int RES, int NV, bool SMALL>
 __global__ __launch_bounds__(1024) void block_norm_kernel(const BlockNormParams p, int waves)
 {
     __shared__ float part[2][1][kMaxWaves];
@@ -38,27 +106,40 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(const BlockNormParams 
     const size_t row_raw = (size_t)blockIdx.x * per_wg + sub;
     const bool have = row_raw < (size_t)p.rows;
     const size_t row = have ? row_raw : p.rows - 1;                 // waves past the last row read it again and store nothing
-    const int t = (wave - first) * 64 + (int)lane, threads = waves * 64;
+    const Place<NV, SMALL> at((wave - first) * 64 + (int)lane, waves * 64, p.C);
 
-    float a[NV][8], r[NV][8];
-    int c0[NV], live[NV];
+    Eight<IO> xr[NV], zr[NV];
+    Eight<RES> rr[NV];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-        c0[k] = (t + k * threads) * 8;
-        live[k] = min(max(p.C - c0[k], 0), 8);
-        if (p.x) load8<IO>(p.x, row * p.x_stride + c0[k], live[k], a[k]);
-        if (p.res) load8<RES>(p.res, row * p.res_stride + c0[k], live[k], r[k]);
+        if (p.x) xr[k].template load<SMALL>(p.x, row * p.x_stride + at.c0[k], p.C);
+        if (p.z) zr[k].template load<SMALL>(p.z, row * p.z_stride + at.c0[k], p.C);
+        if (p.res) rr[k].template load<SMALL>(p.res, row * p.res_stride + at.c0[k], p.C);
+    }
+    float w2[NV][8], cs[NV][8], w1[NV][8];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        if (p.post) weights<SMALL>(p.post, at.c0[k], p.C, w2[k]);
+        if (p.scale) weights<SMALL>(p.scale, at.c0[k], p.C, cs[k]);
+        if (p.pre && p.n_out) weights<SMALL>(p.pre, at.c0[k], p.C, w1[k]);
+    }
+    float r[NV][8];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        if (p.res) rr[k].get(r[k], at.skip[k]);
         else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) r[k][j] = 0.f;
         }
     }
     if (p.x) {
-        if (p.z) {
+        float a[NV][8];
 #pragma unroll
-            for (int k = 0; k < NV; ++k) {
+        for (int k = 0; k < NV; ++k) {
+            xr[k].get(a[k], at.skip[k]);
+            if (p.z) {
                 float z[8];
-                load8<IO>(p.z, row * p.z_stride + c0[k], live[k], z);
+                zr[k].get(z, at.skip[k]);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) a[k][j] *= z[j] * sigmoid(z[j]);
             }
@@ -75,18 +156,15 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(const BlockNormParams 
         }
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            float w[8], c[8];
-            if (p.post) load8<SSMV_F32>(p.post, c0[k], live[k], w);
-            if (p.scale) load8<SSMV_F32>(p.scale, c0[k], live[k], c);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 float v = a[k][j];
-                if (p.post) v = v * scale * w[j];
+                if (p.post) v = v * scale * w2[k][j];
                 v *= p.alpha;
-                if (p.scale) v *= c[j];
+                if (p.scale) v *= cs[k][j];
                 r[k][j] += v;
             }
-            if (p.r_out && have) store8<RES>(p.r_out, row * p.r_stride + c0[k], live[k], r[k]);
+            if (p.r_out && have) put<RES, SMALL>(p.r_out, row * p.r_stride + at.c0[k], at.skip[k], p.C, r[k]);
         }
     }
     if (!p.n_out) return;
@@ -99,216 +177,267 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(const BlockNormParams 
     const float scale = rsqrtf(ss[0] / (float)p.C + p.eps);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-        float w[8];
-        if (p.pre) load8<SSMV_F32>(p.pre, c0[k], live[k], w);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) r[k][j] = p.pre ? r[k][j] * scale * w[j] : r[k][j] * scale;
-        if (have) store8<IO>(p.n_out, row * p.n_stride + c0[k], live[k], r[k]);
+        for (int j = 0; j < 8; ++j) r[k][j] = p.pre ? r[k][j] * scale * w1[k][j] : r[k][j] * scale;
+        if (have) put<IO, SMALL>(p.n_out, row * p.n_stride + at.c0[k], at.skip[k], p.C, r[k]);
     }
 }
 
-// With g = dn * pre_wgt and the row's scales rho (of r) and sigma (of a):
-//   D = dr + rho (g - r rho^2 mean(g r))            = dres
-//   dp = D alpha ch_scale,  g2 = dp post_wgt,  da = sigma (g2 - a sigma^2 mean(g2 a))
-//   dx = da silu(z),  dz = da x silu'(z);   dpre = sum dn r rho,  dscale = sum D alpha p,  dpost = sum dp a sigma over the rows.
-// a, p and r are formed again from the inputs, which have to be read anyway.  A workgroup walks over rows; the sums of the vectors stay in registers, one set a
-// thread, and go to `partial` at the end, where a second launch adds them in a fixed order.
-template <int IO, int RES, int NV>
-__global__ __launch_bounds__(1024) void block_norm_backward_kernel(const BlockNormGradParams p, int waves)
+// With g = dn * pre_wgt, k = alpha ch_scale post_wgt and the row's scales rho (of r) and sigma (of a):
+//   r = res + sigma k a,   D = dr + rho (g - r rho^2 mean(g r))                 = dres
+//   da = sigma (D k - a sigma^2 mean(D k a)),   dx = da silu(z),  dz = da x silu'(z)
+//   dpre = sum dn rho r;  with S = sum D sigma a:  dscale = alpha post_wgt S,  dpost = alpha ch_scale S                 (sums over the rows)
+// a and r are formed again from the inputs, which have to be read anyway.  A workgroup walks over rows, the next one's values on their way while it works on this one's;
+// k, pre_wgt and the two sums of a thread's channels stay in registers.  The sums go to `partial` at the end, where a second launch adds them in a fixed order.
+template <int IO, int RES, int NV, int MAXW, bool SMALL>
+__global__ __launch_bounds__(64 * MAXW) void block_norm_backward_kernel(const BlockNormGradParams p, int waves)
 {
     __shared__ float part[2][3][2][kMaxWaves];                      // of even and odd rows: one barrier lies between any two uses of the same
     const unsigned lane = threadIdx.x & 63u;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), sub = wave / waves, first = sub * waves;
     const int per_wg = (int)(blockDim.x >> 6) / waves;
-    const int t = (wave - first) * 64 + (int)lane, threads = waves * 64;
+    const Place<NV, SMALL> at((wave - first) * 64 + (int)lane, waves * 64, p.C);
     const float inv = 1.f / (float)p.C;
-    int c0[NV], live[NV];
-    float sum_pre[NV][8], sum_scale[NV][8], sum_post[NV][8];
+    float sum_pre[NV][8], S[NV][8], kk[NV][8], w1[NV][8];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-        c0[k] = (t + k * threads) * 8;
-        live[k] = min(max(p.C - c0[k], 0), 8);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum_pre[k][j] = sum_scale[k][j] = sum_post[k][j] = 0.f;
+        for (int j = 0; j < 8; ++j) {
+            sum_pre[k][j] = S[k][j] = 0.f;
+            kk[k][j] = p.alpha;
+            w1[k][j] = 1.f;
+        }
+        if (p.pre) weights<SMALL>(p.pre, at.c0[k], p.C, w1[k]);
+        float w[8];
+        if (p.scale) {
+            weights<SMALL>(p.scale, at.c0[k], p.C, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) kk[k][j] *= w[j];
+        }
+        if (p.post) {
+            weights<SMALL>(p.post, at.c0[k], p.C, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) kk[k][j] *= w[j];
+        }
     }
+    struct Row {
+        Eight<IO> x[NV], z[NV], dn[NV];
+        Eight<RES> res[NV], dr[NV];
+    } next;
+    auto fetch = [&](Row &f, int row_raw) {
+        const size_t row = min(row_raw, p.rows - 1);                // past the last row: that one again
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            if (p.x) f.x[k].template load<SMALL>(p.x, row * p.x_stride + at.c0[k], p.C);
+            if (p.z) f.z[k].template load<SMALL>(p.z, row * p.z_stride + at.c0[k], p.C);
+            if (p.res) f.res[k].template load<SMALL>(p.res, row * p.res_stride + at.c0[k], p.C);
+            if (p.dn) f.dn[k].template load<SMALL>(p.dn, row * p.dn_stride + at.c0[k], p.C);
+            if (p.dr) f.dr[k].template load<SMALL>(p.dr, row * p.dr_stride + at.c0[k], p.C);
+        }
+    };
     const int step = (int)gridDim.x * per_wg;
+    fetch(next, (int)blockIdx.x * per_wg + sub);
     for (int base = (int)blockIdx.x * per_wg, odd = 0; base < p.rows; base += step, odd ^= 1) {    // the same count for all waves of the workgroup
         const bool have = base + sub < p.rows;
         const size_t row = have ? base + sub : p.rows - 1;
-        float a[NV][8], r[NV][8], pv[NV][8];
-        float ss[1] = {0.f};
+        const Row cur = next;
+        if (base + step < p.rows) fetch(next, base + step + sub);
+        float a[NV][8], r[NV][8], d[NV][8];
+        float sigma = 1.f;
+        if (p.x) {
+            float ss[1] = {0.f};
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            if (p.x) load8<IO>(p.x, row * p.x_stride + c0[k], live[k], a[k]);
-            if (p.z) {
-                float z[8];
-                load8<IO>(p.z, row * p.z_stride + c0[k], live[k], z);
+            for (int k = 0; k < NV; ++k) {
+                cur.x[k].get(a[k], at.skip[k]);
+                if (p.z) {
+                    float z[8];
+                    cur.z[k].get(z, at.skip[k]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) a[k][j] *= z[j] * sigmoid(z[j]);
-            }
-            if (p.post)
+                    for (int j = 0; j < 8; ++j) a[k][j] *= z[j] * sigmoid(z[j]);
+                }
 #pragma unroll
                 for (int j = 0; j < 8; ++j) ss[0] = fmaf(a[k][j], a[k][j], ss[0]);
+            }
+            if (p.post) {
+                row_sums<1>(ss, part[odd][0], first, waves, wave, lane);
+                sigma = rsqrtf(ss[0] * inv + p.eps);
+            }
         }
-        float sigma = 1.f;
-        if (p.post) {
-            row_sums<1>(ss, part[odd][0], first, waves, wave, lane);
-            sigma = rsqrtf(ss[0] * inv + p.eps);
-        }
-        float rs[2] = {0.f, 0.f};                                  // sum r^2, sum g r
-        float dn[NV][8], d[NV][8];
+        const float sig = have ? sigma : 0.f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            float w[8];
-            if (p.res) load8<RES>(p.res, row * p.res_stride + c0[k], live[k], r[k]);
+            if (p.res) cur.res[k].get(r[k], at.skip[k]);
             else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) r[k][j] = 0.f;
             }
-            if (p.x) {
-                float c[8];
-                if (p.post) load8<SSMV_F32>(p.post, c0[k], live[k], w);
-                if (p.scale) load8<SSMV_F32>(p.scale, c0[k], live[k], c);
+            if (p.x)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    pv[k][j] = p.post ? a[k][j] * sigma * w[j] : a[k][j];
-                    float v = pv[k][j] * p.alpha;
-                    if (p.scale) v *= c[j];
-                    r[k][j] += v;
-                }
-            }
-            if (p.dn) {
-                if (p.pre) load8<SSMV_F32>(p.pre, c0[k], live[k], w);
-                load8<IO>(p.dn, row * p.dn_stride + c0[k], live[k], dn[k]);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float g = p.pre ? dn[k][j] * w[j] : dn[k][j];
-                    rs[0] = fmaf(r[k][j], r[k][j], rs[0]);
-                    rs[1] = fmaf(g, r[k][j], rs[1]);
-                }
-            }
-            if (p.dr) load8<RES>(p.dr, row * p.dr_stride + c0[k], live[k], d[k]);
+                for (int j = 0; j < 8; ++j) r[k][j] = fmaf(a[k][j], sigma * kk[k][j], r[k][j]);
+            if (p.dr) cur.dr[k].get(d[k], at.skip[k]);
             else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) d[k][j] = 0.f;
             }
         }
         if (p.dn) {
-            row_sums<2>(rs, part[odd][1], first, waves, wave, lane);
-            const float rho = rsqrtf(rs[0] * inv + p.eps), back = rho * rho * (rs[1] * inv);
+            float rs[2] = {0.f, 0.f};                              // sum r^2, sum g r
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                float w[8];
-                if (p.pre) load8<SSMV_F32>(p.pre, c0[k], live[k], w);
+                float dn[8];
+                cur.dn[k].get(dn, at.skip[k]);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float g = p.pre ? dn[k][j] * w[j] : dn[k][j];
-                    d[k][j] = fmaf(rho, fmaf(-r[k][j], back, g), d[k][j]);
-                    sum_pre[k][j] = fmaf(have ? dn[k][j] * rho : 0.f, r[k][j], sum_pre[k][j]);
+                    rs[0] = fmaf(r[k][j], r[k][j], rs[0]);
+                    rs[1] = fmaf(dn[j] * w1[k][j], r[k][j], rs[1]);
+                }
+            }
+            row_sums<2>(rs, part[odd][1], first, waves, wave, lane);
+            const float rho = rsqrtf(rs[0] * inv + p.eps), back = rho * rho * (rs[1] * inv), rh = have ? rho : 0.f;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                float dn[8];
+                cur.dn[k].get(dn, at.skip[k]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    d[k][j] = fmaf(rho, fmaf(-r[k][j], back, dn[j] * w1[k][j]), d[k][j]);
+                    sum_pre[k][j] = fmaf(dn[j] * rh, r[k][j], sum_pre[k][j]);
                 }
             }
         }
         if (p.dres && have)
 #pragma unroll
-            for (int k = 0; k < NV; ++k) store8<RES>(p.dres, row * p.dres_stride + c0[k], live[k], d[k]);
-        if (p.x) {
-            float gs[1] = {0.f};
+            for (int k = 0; k < NV; ++k) put<RES, SMALL>(p.dres, row * p.dres_stride + at.c0[k], at.skip[k], p.C, d[k]);
+        if (!p.x) continue;
+        float gs[1] = {0.f};
 #pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                float c[8], w[8];
-                if (p.scale) load8<SSMV_F32>(p.scale, c0[k], live[k], c);
-                if (p.post) load8<SSMV_F32>(p.post, c0[k], live[k], w);
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                S[k][j] = fmaf(d[k][j] * sig, a[k][j], S[k][j]);
+                d[k][j] *= kk[k][j];
+                gs[0] = fmaf(d[k][j], a[k][j], gs[0]);
+            }
+        if (p.post) {
+            row_sums<1>(gs, part[odd][2], first, waves, wave, lane);
+            const float back = sigma * sigma * (gs[0] * inv);
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) d[k][j] = sigma * fmaf(-a[k][j], back, d[k][j]);
+        }
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            if (p.z) {
+                float x[8], z[8], dz[8];
+                cur.x[k].get(x, at.skip[k]);
+                cur.z[k].get(z, at.skip[k]);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    float v = d[k][j] * p.alpha;
-                    if (p.scale) {
-                        sum_scale[k][j] = fmaf(have ? v : 0.f, pv[k][j], sum_scale[k][j]);
-                        v *= c[j];
-                    }
-                    if (p.post) {
-                        sum_post[k][j] = fmaf(have ? v * sigma : 0.f, a[k][j], sum_post[k][j]);
-                        v *= w[j];
-                        gs[0] = fmaf(v, a[k][j], gs[0]);
-                    }
-                    d[k][j] = v;
+                    const float sg = sigmoid(z[j]), s = z[j] * sg;
+                    dz[j] = d[k][j] * x[j] * fmaf(s, 1.f - sg, sg);
+                    d[k][j] *= s;
                 }
+                if (p.dz && have) put<IO, SMALL>(p.dz, row * p.dz_stride + at.c0[k], at.skip[k], p.C, dz);
             }
-            if (p.post) {
-                row_sums<1>(gs, part[odd][2], first, waves, wave, lane);
-                const float back = sigma * sigma * (gs[0] * inv);
-#pragma unroll
-                for (int k = 0; k < NV; ++k)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) d[k][j] = sigma * fmaf(-a[k][j], back, d[k][j]);
-            }
-            if (p.z) {
-#pragma unroll
-                for (int k = 0; k < NV; ++k) {
-                    float x[8], z[8], dz[8];
-                    load8<IO>(p.x, row * p.x_stride + c0[k], live[k], x);
-                    load8<IO>(p.z, row * p.z_stride + c0[k], live[k], z);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float sg = sigmoid(z[j]);
-                        dz[j] = d[k][j] * x[j] * sg * fmaf(z[j], 1.f - sg, 1.f);
-                        d[k][j] *= z[j] * sg;
-                    }
-                    if (p.dz && have) store8<IO>(p.dz, row * p.dz_stride + c0[k], live[k], dz);
-                }
-            }
-            if (p.dx && have)
-#pragma unroll
-                for (int k = 0; k < NV; ++k) store8<IO>(p.dx, row * p.dx_stride + c0[k], live[k], d[k]);
+            if (p.dx && have) put<IO, SMALL>(p.dx, row * p.dx_stride + at.c0[k], at.skip[k], p.C, d[k]);
         }
     }
     if (!p.partial) return;
-    float *to = p.partial + ((size_t)blockIdx.x * per_wg + sub) * 3 * p.C;
+    if (per_wg > 1) {                                               // the rows of the workgroup, in order
+        extern __shared__ __attribute__((aligned(16))) float sums[];     // [2][threads of a row][8 NV]
+        const int t = (wave - first) * 64 + (int)lane, each = waves * 64 * 8 * NV;
+        for (int s = 1; s < per_wg; ++s) {
+            __syncthreads();
+            if (sub == s) {
+#pragma unroll
+                for (int k = 0; k < NV; ++k)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        sums[(k * 8 + j) * waves * 64 + t] = sum_pre[k][j];
+                        sums[each + (k * 8 + j) * waves * 64 + t] = S[k][j];
+                    }
+            }
+            __syncthreads();
+            if (sub == 0) {
+#pragma unroll
+                for (int k = 0; k < NV; ++k)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        sum_pre[k][j] += sums[(k * 8 + j) * waves * 64 + t];
+                        S[k][j] += sums[each + (k * 8 + j) * waves * 64 + t];
+                    }
+            }
+        }
+        if (sub != 0) return;
+    }
+    float *to = p.partial + (size_t)blockIdx.x * 3 * p.C;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-        store8<SSMV_F32>(to, c0[k], live[k], sum_pre[k]);
-        store8<SSMV_F32>(to, (size_t)p.C + c0[k], live[k], sum_scale[k]);
-        store8<SSMV_F32>(to, (size_t)2 * p.C + c0[k], live[k], sum_post[k]);
+        put<SSMV_F32, SMALL>(to, at.c0[k], at.skip[k], p.C, sum_pre[k]);
+        float w[8], v[8];
+        if (p.scale) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = 1.f;
+            if (p.post) weights<SMALL>(p.post, at.c0[k], p.C, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = p.alpha * w[j] * S[k][j];
+            put<SSMV_F32, SMALL>(to, (size_t)p.C + at.c0[k], at.skip[k], p.C, v);
+        }
+        if (p.post) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = 1.f;
+            if (p.scale) weights<SMALL>(p.scale, at.c0[k], p.C, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = p.alpha * w[j] * S[k][j];
+            put<SSMV_F32, SMALL>(to, (size_t)2 * p.C + at.c0[k], at.skip[k], p.C, v);
+        }
     }
 }
 
-// 64 columns side by side, 16 parts of the rows; the parts are added in order
+// 32 columns side by side, 32 strands of the parts; the strands are added in order
 __global__ __launch_bounds__(1024) void column_sums_kernel(const float *partial, int parts, int C, ColumnSums to)
 {
-    __shared__ float acc[16][64];
-    const int c = (int)blockIdx.x * 64 + (int)(threadIdx.x & 63), k = blockIdx.y, w = threadIdx.x >> 6;
+    __shared__ float acc[32][32];
+    const int col = threadIdx.x & 31, w = threadIdx.x >> 5, c = (int)blockIdx.x * 32 + col, k = blockIdx.y;
     if (!to.out[k]) return;
     float s = 0.f;
-    if (c < C)
-        for (int r = w; r < parts; r += 16) s += partial[((size_t)r * gridDim.y + k) * C + c];
-    acc[w][threadIdx.x & 63] = s;
+    if (c < C) {
+        const float *from = partial + (size_t)k * C + c;
+        const size_t row = (size_t)gridDim.y * C;
+#pragma unroll 4
+        for (int r = w; r < parts; r += 32) s += from[r * row];
+    }
+    acc[w][col] = s;
     __syncthreads();
     if (w != 0 || c >= C) return;
-    for (int j = 1; j < 16; ++j) s += acc[j][threadIdx.x];
+    for (int j = 1; j < 32; ++j) s += acc[j][col];
     if (to.over[k]) s = to.over[k][c] == 0.f ? 0.f : s / to.over[k][c];
     to.out[k][c] = s;
 }
 
-// waves of a row, and vectors of 8 channels a thread: one, or two where a workgroup has not the threads for that
+// Waves of a row, vectors of 8 channels a thread - one, or two where `most_waves` are too few for that -, and rows of a workgroup of about `waves_wg` waves.
 struct RowShape {
     int nv, waves, per_wg;
 };
-RowShape row_shape(int C)
+RowShape row_shape(int C, int most_waves, int waves_wg)
 {
     const int vectors = (C + 7) / 8;
     RowShape s;
-    s.nv = vectors > 64 * kMaxWaves ? 2 : 1;
+    s.nv = vectors > 64 * most_waves ? 2 : 1;
     s.waves = (vectors + 64 * s.nv - 1) / (64 * s.nv);
-    s.per_wg = s.waves >= 4 ? 1 : 4 / s.waves;
+    s.per_wg = s.waves >= waves_wg ? 1 : waves_wg / s.waves;
     return s;
 }
 
 template <int IO, int RES>
 int launch_forward(const BlockNormParams &p, hipStream_t stream)
 {
-    const RowShape s = row_shape(p.C);
+    const RowShape s = row_shape(p.C, kMaxWaves, 4);
     const dim3 grid((unsigned)((p.rows + s.per_wg - 1) / s.per_wg)), block(64 * s.waves * s.per_wg);
-    if (s.nv == 1) hipLaunchKernelGGL((block_norm_kernel<IO, RES, 1>), grid, block, 0, stream, p, s.waves);
-    else hipLaunchKernelGGL((block_norm_kernel<IO, RES, 2>), grid, block, 0, stream, p, s.waves);
+    if (p.C < 8) hipLaunchKernelGGL((block_norm_kernel<IO, RES, 1, true>), grid, block, 0, stream, p, s.waves);
+    else if (s.nv == 1) hipLaunchKernelGGL((block_norm_kernel<IO, RES, 1, false>), grid, block, 0, stream, p, s.waves);
+    else hipLaunchKernelGGL((block_norm_kernel<IO, RES, 2, false>), grid, block, 0, stream, p, s.waves);
     return (int)hipGetLastError();
 }
 
@@ -316,25 +445,29 @@ template <int IO, int RES>
 int launch_backward(const BlockNormGradParams &q, hipStream_t stream)
 {
     BlockNormGradParams p = q;
-    const RowShape s = row_shape(p.C);
-    // no more partial sums than the workspace has room for
+    const RowShape s = row_shape(p.C, 12, 8);                       // more waves leave a thread 128 registers, too few for the loop
     int wgs = (p.rows + s.per_wg - 1) / s.per_wg;
-    const int most = norm_parts(p.rows) / s.per_wg > 0 ? norm_parts(p.rows) / s.per_wg : 1;
+    const int most = s.nv == 1 && s.waves <= 8 ? kNormParts : kNormParts / 2;     // two workgroups of 8 waves run on a compute unit, one of more
     if (wgs > most) wgs = most;
     const dim3 grid((unsigned)wgs), block(64 * s.waves * s.per_wg);
-    if (s.nv == 1) hipLaunchKernelGGL((block_norm_backward_kernel<IO, RES, 1>), grid, block, 0, stream, p, s.waves);
-    else hipLaunchKernelGGL((block_norm_backward_kernel<IO, RES, 2>), grid, block, 0, stream, p, s.waves);
+    const size_t lds = s.per_wg > 1 && p.partial ? (size_t)2 * s.waves * 64 * 8 * sizeof(float) : 0;
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, lds, stream, p, s.waves); };
+    if (p.C < 8) go(block_norm_backward_kernel<IO, RES, 1, 8, true>);
+    else if (s.nv == 1 && s.waves <= 8) go(block_norm_backward_kernel<IO, RES, 1, 8, false>);
+    else if (s.nv == 1) go(block_norm_backward_kernel<IO, RES, 1, 12, false>);
+    else if (s.waves <= 8) go(block_norm_backward_kernel<IO, RES, 2, 8, false>);
+    else go(block_norm_backward_kernel<IO, RES, 2, 16, false>);
     const int e = (int)hipGetLastError();
     if (e != 0 || !p.partial) return e;
     const ColumnSums to{{p.dpre, p.dscale, p.dpost}, {nullptr, nullptr, nullptr}};
-    return launch_column_sums(p.partial, wgs * s.per_wg, p.C, to, stream);
+    return launch_column_sums(p.partial, wgs, p.C, to, stream);
 }
 
 }  // namespace
 
 int launch_column_sums(const float *partial, int parts, int C, const ColumnSums &to, hipStream_t stream)
 {
-    hipLaunchKernelGGL(column_sums_kernel, dim3((unsigned)((C + 63) / 64), 3), dim3(1024), 0, stream, partial, parts, C, to);
+    hipLaunchKernelGGL(column_sums_kernel, dim3((unsigned)((C + 31) / 32), 3), dim3(1024), 0, stream, partial, parts, C, to);
     return (int)hipGetLastError();
 }
 

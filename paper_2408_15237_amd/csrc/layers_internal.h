@@ -83,9 +83,9 @@ struct ColumnSums {
 };
 int launch_column_sums(const float *partial, int parts, int C, const ColumnSums &to, hipStream_t stream);
 
-// Rows' weight gradients are summed by so many workgroups (threads of a row: see norm_threads).
+// The gradients of vectors are summed over the rows by at most so many workgroups: two on every compute unit.
 constexpr int kNormParts = 512;
-inline int norm_parts(int rows) { return rows < kNormParts ? (rows + 3) / 4 * 4 : kNormParts; }     // a workgroup holds up to four rows
+inline int norm_parts(int rows) { return rows < kNormParts ? rows : kNormParts; }
 
 // How the recurrence is laid on the chip.  A workgroup takes 512 threads; `lanes` lanes of a wave lie side by side over the channels (two bf16
 // channels a lane, or one fp32), the others over the tokens, 8 a lane: 64 * 64 / lanes tokens a tile.
