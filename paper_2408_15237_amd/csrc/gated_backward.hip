@@ -1,4 +1,6 @@
 // The gradients of the gated linear recurrence.
+#include <type_traits>
+
 #include "gated_common.h"
 
 namespace ssmv {
@@ -6,154 +8,186 @@ namespace {
 
 // h_t = a_t h_{t-1} + v_t,  y_t = h_t silu(z_t).  With g_t = dy_t silu(z_t) and c the gradient that flows into the state from the tokens behind (dh_out at the end):
 //   G_t = g_t + c,   c <- a_t G_t          (dh_in at the front)
-//   MIX, a = r, m = 1 - r, r = sigmoid(f), u = i x:    df = G r (1 - r) (h_{t-1} - u)
+//   MIX, a = r, m = 1 - r, r = sigmoid(f), u = sigmoid(i) x:      df = G r (1 - r) (h_{t-1} - u)
 //   LRU, a = e^-s, s = -A r, m = sqrt(1 - a^2), v = m u:
 //     E = s dL/ds = G s a (v a / m^2 - h_{t-1}),   df = E (1 - r),   dA = sum E / A        (E falls with sqrt(s) as s goes to 0)
-//   dx = G m i,   di = G v (1 - i),   dz = dy h silu'(z)
+//   dx = G m sigmoid(i),   di = G v (1 - sigmoid(i)),   dz = dy h silu'(z)
 // The tiles from the last to the first.  A lane's run is the pair (P, H) of the forward pass and, from its last token to its first, the pair (P, R): c <- P c + R, with the
-// same product.  Lanes and waves combine both in one exchange: forwards inside 64 tokens, from the state that the forward pass left ahead of them, backwards through the whole tile.
+// same product.  Runs and waves combine both in one exchange: forwards inside 64 tokens, from the state that the forward pass left ahead of them, backwards through the whole
+// tile.  What the gradients take of the gates is formed on the first walk, so that nothing of a token is worked out twice.
 // OUT false: only the pairs (P, R) of whole segments, of all but the first.
-template <int IO, int CL, bool LRU, bool OUT>
-__global__ __launch_bounds__(64 * kGatedWaves) void gated_backward_kernel(const GatedGradParams p)
+template <int IO, int W, bool LRU, bool HASI, bool HASZ, bool OUT>
+__global__ __launch_bounds__(64 * W) void gated_backward_kernel(const GatedGradParams p)
 {
-    using Ln = GatedLane<IO, CL>;
-    constexpr int CH = Ln::CH, G = Ln::G, T = Ln::T, K = kGatedRun, W = kGatedWaves;
-    constexpr int BW = SSMV_GATED_TILE / (G * K);                   // waves that share a state of the forward pass
-    static_assert(BW >= 1 && BW * G * K == SSMV_GATED_TILE && T % SSMV_GATED_TILE == 0, "tile");
-    __shared__ __attribute__((aligned(16))) float pairs[2][W][CL][3 * CH];
-    const unsigned lane = threadIdx.x & 63u, cl = lane % CL, grp = lane / CL;
+    using Ln = GatedLane<IO>;
+    constexpr int CH = Ln::CH, T = W * kWaveTokens, K = kRun;
+    static_assert(W % kBlockWaves == 0, "tiles are whole blocks of 64 tokens");
+    __shared__ __attribute__((aligned(16))) float pairs[2][W][kLanes][3 * CH];
+    __shared__ __attribute__((aligned(16))) uint32_t ahead[OUT ? 3 + HASI + HASZ : 2 + HASZ][K][W][64];       // the next tile's values, on their way: each wave's own
+    const unsigned lane = threadIdx.x & 63u, cl = lane % kLanes, run = lane / kLanes;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int c0 = (int)xcd_contiguous(blockIdx.x, gridDim.x) * Ln::CW + (int)cl * CH, live = min(max(p.C - c0, 0), CH);
-    const int seg = OUT ? blockIdx.y : blockIdx.y + 1;
+    const int first = (int)xcd_contiguous(blockIdx.x, gridDim.x) * Ln::CW, seg = OUT ? blockIdx.y : blockIdx.y + 1;
+    const Ln ln(first + (int)cl * CH, p.C);
     int b = blockIdx.z;
-    if (p.seq_len && p.batch > 1 && p.batch <= 64) b = zth_longest(p.seq_len, p.batch, b, lane);
+    if (p.seq_len && p.batch > 1 && p.batch <= 64) b = __builtin_amdgcn_readfirstlane(zth_longest(p.seq_len, p.batch, b, lane));
     const int all = p.seq_len ? min(max(p.seq_len[b], 0), p.L) : p.L;
     const int from = seg * p.seg_len, len = min(all, from + p.seg_len);
     const bool have = seg == 0 || from < all;                       // segments behind the sequence's end: nothing but zeros in the sums
-    const size_t seg0 = (size_t)b * p.seg_count * p.C + c0;
+    const size_t seg0 = (size_t)b * p.seg_count * p.C;
     if (!OUT && !have) return;
 
     float carry[CH], prod[CH], rate[CH], fb[CH], ib[CH], sumA[CH], sumF[CH], sumI[CH];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        carry[c] = sumA[c] = sumF[c] = sumI[c] = 0.f;
+        carry[c] = sumA[c] = sumF[c] = sumI[c] = rate[c] = fb[c] = ib[c] = 0.f;
         prod[c] = 1.f;
-        rate[c] = LRU && c < live ? decay_exponent(p.A[c0 + c]) : 0.f;
-        fb[c] = p.f_bias && c < live ? p.f_bias[c0 + c] : 0.f;
-        ib[c] = p.i_bias && c < live ? p.i_bias[c0 + c] : 0.f;
     }
+    if (LRU) {
+        ln.floats(p.A, rate);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) rate[c] = decay_exponent(rate[c]);
+    }
+    if (p.f_bias) ln.floats(p.f_bias, fb);
+    if (HASI && p.i_bias) ln.floats(p.i_bias, ib);
     if (have && (OUT || len == all)) {
-        if (p.dh_out) load_channels<CH>(p.dh_out + (size_t)b * p.C + c0, live, carry);
+        if (p.dh_out) ln.floats(p.dh_out + (size_t)b * p.C, carry);
         if (OUT)
             for (int j = (all + p.seg_len - 1) / p.seg_len - 1; j > seg; --j) {      // the last segment's R has dh_out in it
                 float sp[CH], sr[CH];
-                load_channels<CH>(p.seg_p + seg0 + (size_t)j * p.C, live, sp);
-                load_channels<CH>(p.seg_r + seg0 + (size_t)j * p.C, live, sr);
+                ln.floats(p.seg_p + seg0 + (size_t)j * p.C, sp);
+                ln.floats(p.seg_r + seg0 + (size_t)j * p.C, sr);
                 const bool end = (j + 1) * (size_t)p.seg_len >= (size_t)all;
 #pragma unroll
                 for (int c = 0; c < CH; ++c) carry[c] = end ? sr[c] : fmaf(sp[c], carry[c], sr[c]);
             }
     }
 
-    const size_t tok0 = (size_t)b * p.L, blocks = (p.L + SSMV_GATED_TILE - 1) / SSMV_GATED_TILE;
-    const int run0 = (wave * G + (int)grp) * K;
-    auto offset = [&](size_t stride) { return (unsigned)((grp * K * (unsigned)stride + (unsigned)c0) * Ln::ES); };
-    const unsigned ox = offset(p.x_stride), of = offset(p.f_stride), oi = offset(p.i_stride), oz = offset(p.z_stride), oy = offset(p.dy_stride);
-    const unsigned odx = offset(p.dx_stride), odf = offset(p.df_stride), odi = offset(p.di_stride), odz = offset(p.dz_stride);
-    const int tiles = have ? (len - from + T - 1) / T : 0;
-    for (int n = tiles - 1, buf = 0; n >= 0; --n, buf ^= 1) {
-        const int t0 = from + n * T, t = t0 + run0;
-        const size_t at = tok0 + t0 + wave * G * K;
-        uint32_t rx[K], rf[K], ri[K], rz[K], ry[K];
-        Ln::load_run(rf, p.f, p.f_stride, at, of, live, t, len);
-        Ln::load_run(ry, p.dy, p.dy_stride, at, oy, live, t, len);
-        if (p.z) Ln::load_run(rz, p.z, p.z_stride, at, oz, live, t, len);
-        float begin[CH];
-        if constexpr (OUT) {
-            Ln::load_run(rx, p.x, p.x_stride, at, ox, live, t, len);
-            if (p.i) Ln::load_run(ri, p.i, p.i_stride, at, oi, live, t, len);
-            // of the block of 64 tokens; one that has none is not looked at
-            const int first = t / SSMV_GATED_TILE * SSMV_GATED_TILE;
-#pragma unroll
-            for (int c = 0; c < CH; ++c) begin[c] = 0.f;
-            if (first < len) load_channels<CH>(p.states + ((size_t)b * blocks + t / SSMV_GATED_TILE) * p.C + c0, live, begin);
-        }
-        float a[K][CH], v[OUT ? K : 1][CH], g[K][CH];
+    const size_t blocks = (p.L + SSMV_GATED_TILE - 1) / SSMV_GATED_TILE;
+    const int wave0 = wave * kWaveTokens, run0 = wave0 + (int)run * K;
+    // the last tile, where it is not whole (all of them of a row of one bf16 channel), then whole ones
+    const int n = have ? len - from : 0, whole = p.C >= CH ? n - n % T : 0;
+    int t0 = from + (n + T - 1) / T * T - T;
+    const size_t tok0 = (size_t)b * p.L + wave0 + t0;               // of a tile that is there, but where there is none
+    Walk<IO> wx(p.x, p.x_stride, tok0, run, ln), wf(p.f, p.f_stride, tok0, run, ln), wi(p.i, p.i_stride, tok0, run, ln), wz(p.z, p.z_stride, tok0, run, ln),
+        wy(p.dy, p.dy_stride, tok0, run, ln);
+    Walk<IO> wdx(p.dx, p.dx_stride, tok0, run, ln), wdf(p.df, p.df_stride, tok0, run, ln), wdi(p.di, p.di_stride, tok0, run, ln), wdz(p.dz, p.dz_stride, tok0, run, ln);
+    uint32_t rx[K], rf[K], ri[K], rz[K], ry[K];
+    float block[CH];                                                // the state ahead of the lane's block of 64 tokens
+    auto each = [&](auto &&fn) {                                    // the tensors of a tile
+        fn(wf, rf, 0);
+        fn(wy, ry, 1);
+        if (HASZ) fn(wz, rz, 2);
+        if (OUT) fn(wx, rx, 2 + HASZ);
+        if (OUT && HASI) fn(wi, ri, 3 + HASZ);
+    };
+    // of a block that has no token the last block's, which nothing comes of
+    auto state = [&](int t0) { if (OUT) ln.floats(p.states + ((size_t)b * blocks + min(t0 + wave0, len - 1) / SSMV_GATED_TILE) * p.C, block); };
+    auto fetch_tail = [&](int t0) {
+        state(t0);
+        each([&](auto &w, uint32_t (&r)[K], int) {
+            w.load_tail(r, t0 + wave0, run, len, ln);
+            w.move(-T);
+        });
+    };
+    auto prefetch = [&](int t0) {
+        state(t0);
+        each([&](auto &w, uint32_t (&)[K], int i) {
+            w.prefetch(&ahead[i][0][wave][0], W * 64);
+            w.move(-T);
+        });
+    };
+    auto tile = [&](auto tail, int t0, int buf, auto &&next) {
+        constexpr bool TAIL = decltype(tail)::value;
+        const int t = t0 + run0;
+        float a[K][CH], g[K][CH], v[OUT ? K : 1][CH], zz[OUT ? K : 1][CH];
+        float e0[OUT ? K : 1][CH], e1[OUT ? K : 1][CH], e2[OUT ? K : 1][CH], ex[OUT ? K : 1][CH], ei[OUT ? K : 1][CH], begin[CH];
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             float f[CH], x[CH], i[CH], z[CH], dy[CH];
             Ln::decode(rf[k], f);
             Ln::decode(ry[k], dy);
             if (OUT) Ln::decode(rx[k], x);
-            if (OUT && p.i) Ln::decode(ri[k], i);
-            if (p.z) Ln::decode(rz[k], z);
-            const bool is = t + k < len;
+            if (OUT && HASI) Ln::decode(ri[k], i);
+            if (HASZ) Ln::decode(rz[k], z);
+            constexpr int O = OUT ? 1 : 0;
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                float m;
-                if constexpr (LRU) {
-                    const float q = rate[c] * sigmoid(f[c] + fb[c]);
+                float r, nr, q = 0.f, m = 0.f, m2 = 0.f;
+                sigmoids(f[c] + fb[c], r, nr);
+                a[k][c] = r;
+                if (LRU) {
+                    q = rate[c] * r;
                     a[k][c] = __builtin_amdgcn_exp2f(q);
-                    if (OUT) m = __builtin_amdgcn_sqrtf(one_minus_square(q, a[k][c]));
-                } else {
-                    sigmoids(f[c] + fb[c], a[k][c], m);
+                }
+                g[k][c] = dy[c];
+                if (HASZ) {
+                    const float sg = sigmoid(z[c]), s = z[c] * sg;
+                    g[k][c] = dy[c] * s;
+                    if (OUT) zz[O * k][c] = dy[c] * fmaf(s, 1.f - sg, sg);
                 }
                 if (OUT) {
-                    float w = m * x[c];
-                    if (p.i) w *= sigmoid(i[c] + ib[c]);
-                    v[OUT ? k : 0][c] = is ? w : 0.f;
+                    float si = 1.f, ni = 0.f;
+                    if (HASI) sigmoids(i[c] + ib[c], si, ni);
+                    const float u = HASI ? x[c] * si : x[c];
+                    if (LRU) {
+                        m2 = one_minus_square(q, a[k][c]);
+                        m = __builtin_amdgcn_sqrtf(m2);
+                    } else {
+                        m = nr;
+                    }
+                    const float w = m * u;
+                    v[O * k][c] = w;
+                    ex[O * k][c] = HASI ? m * si : m;
+                    if (HASI) ei[O * k][c] = w * ni;
+                    if (LRU) {                                      // E = G e0 (e1 - h)
+                        e0[O * k][c] = (-kLn2 * q) * a[k][c];
+                        e1[O * k][c] = w * a[k][c] * __builtin_amdgcn_rcpf(fmaxf(m2, 1e-37f));
+                        e2[O * k][c] = nr;
+                    } else {                                        // df = G e0 (h - e1)
+                        e0[O * k][c] = r * nr;
+                        e1[O * k][c] = u;
+                    }
                 }
-                a[k][c] = is ? a[k][c] : 1.f;
-                const float d = p.z ? dy[c] * (z[c] * sigmoid(z[c])) : dy[c];
-                g[k][c] = is ? d : 0.f;
             }
         }
-        float P[CH], H[CH], R[CH], Pf[CH], Hf[CH], Pr[CH], Rr[CH];   // of the run; exclusive over the wave's runs before and behind
+#pragma unroll
+        for (int c = 0; c < CH; ++c) begin[c] = block[c];
+        if (TAIL) {                                                 // tokens that are none: nothing flows into them, and through them as it is
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int c = 0; c < CH; ++c) {
+                    const bool is = t + k < len;
+                    a[k][c] = is ? a[k][c] : 1.f;
+                    g[k][c] = is ? g[k][c] : 0.f;
+                    if (OUT) {
+                        v[OUT ? k : 0][c] = is ? v[OUT ? k : 0][c] : 0.f;
+                        e0[OUT ? k : 0][c] = is ? e0[OUT ? k : 0][c] : 0.f;
+                        if (HASI) ei[OUT ? k : 0][c] = is ? ei[OUT ? k : 0][c] : 0.f;
+                    }
+                }
+        }
+        next();
+        float Pf[CH], Hf[CH], Pr[CH], Rr[CH], Pt[CH], Ht[CH], Rt[CH];
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            P[c] = a[0][c];
-            H[c] = OUT ? v[0][c] : 0.f;
+            float P = a[0][c], H = OUT ? v[0][c] : 0.f, R = a[K - 1][c] * g[K - 1][c];
 #pragma unroll
             for (int k = 1; k < K; ++k) {
-                P[c] *= a[k][c];
-                if (OUT) H[c] = fmaf(a[k][c], H[c], v[OUT ? k : 0][c]);
+                P *= a[k][c];
+                if (OUT) H = fmaf(a[k][c], H, v[OUT ? k : 0][c]);
+                R = a[K - 1 - k][c] * (g[K - 1 - k][c] + R);
             }
-            R[c] = a[K - 1][c] * g[K - 1][c];
-#pragma unroll
-            for (int k = K - 2; k >= 0; --k) R[c] = a[k][c] * (g[k][c] + R[c]);
-            Pf[c] = Pr[c] = 1.f;
-            Hf[c] = Rr[c] = 0.f;
-            if constexpr (G > 1) {
-                float P2 = P[c];
-#pragma unroll
-                for (int d = CL; d < 64; d *= 2) {
-                    const float p1 = __shfl_up(P[c], d), h1 = __shfl_up(H[c], d), p2 = __shfl_down(P2, d), r2 = __shfl_down(R[c], d);
-                    if ((int)lane >= d) {
-                        H[c] = fmaf(P[c], h1, H[c]);
-                        P[c] *= p1;
-                    }
-                    if ((int)lane + d < 64) {
-                        R[c] = fmaf(P2, r2, R[c]);
-                        P2 *= p2;
-                    }
-                }
-                const float p1 = __shfl_up(P[c], CL), h1 = __shfl_up(H[c], CL), p2 = __shfl_down(P2, CL), r2 = __shfl_down(R[c], CL);
-                Pf[c] = grp > 0 ? p1 : 1.f;
-                Hf[c] = grp > 0 ? h1 : 0.f;
-                Pr[c] = grp < G - 1 ? p2 : 1.f;
-                Rr[c] = grp < G - 1 ? r2 : 0.f;
-            }
+            combine_forward(P, H, run, Pf[c], Hf[c], Pt[c], Ht[c]);
+            combine_backward(P, R, run, Pr[c], Rr[c], Rt[c]);
         }
-        if (grp == G - 1) {
+        if (run == 0) {
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                pairs[buf][wave][cl][c] = P[c];
-                pairs[buf][wave][cl][CH + c] = H[c];
+                pairs[buf][wave][cl][c] = Pt[c];
+                pairs[buf][wave][cl][CH + c] = Rt[c];
+                pairs[buf][wave][cl][2 * CH + c] = Ht[c];
             }
-        }
-        if (grp == 0) {
-#pragma unroll
-            for (int c = 0; c < CH; ++c) pairs[buf][wave][cl][2 * CH + c] = R[c];
         }
         __syncthreads();
         float flow[CH];                                             // into the lane's last token
@@ -161,142 +195,145 @@ __global__ __launch_bounds__(64 * kGatedWaves) void gated_backward_kernel(const 
         for (int w = W - 1; w >= 0; --w) {
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                if (w == wave) flow[c] = carry[c];
+                flow[c] = w == wave ? carry[c] : w == W - 1 ? 0.f : flow[c];
                 const float pw = pairs[buf][w][cl][c];
-                carry[c] = fmaf(pw, carry[c], pairs[buf][w][cl][2 * CH + c]);
+                carry[c] = fmaf(pw, carry[c], pairs[buf][w][cl][CH + c]);
                 if (!OUT) prod[c] *= pw;
             }
         }
         if constexpr (OUT) {
+            for (int w = wave / kBlockWaves * kBlockWaves; w < wave; ++w)
 #pragma unroll
-            for (int c = 0; c < CH; ++c) flow[c] = fmaf(Pr[c], flow[c], Rr[c]);
-            if constexpr (BW > 1) {
-                for (int w = wave / BW * BW; w < wave; ++w)
+                for (int c = 0; c < CH; ++c) begin[c] = fmaf(pairs[buf][w][cl][c], begin[c], pairs[buf][w][cl][2 * CH + c]);
 #pragma unroll
-                    for (int c = 0; c < CH; ++c) begin[c] = fmaf(pairs[buf][w][cl][c], begin[c], pairs[buf][w][cl][CH + c]);
+            for (int c = 0; c < CH; ++c) {
+                flow[c] = fmaf(Pr[c], flow[c], Rr[c]);
+                begin[c] = fmaf(Pf[c], begin[c], Hf[c]);
             }
-#pragma unroll
-            for (int c = 0; c < CH; ++c) begin[c] = fmaf(Pf[c], begin[c], Hf[c]);
-            float before[K][CH];                                    // the state ahead of every token
+            // e1 becomes what E or df takes of the state ahead of the token, zz the gradient of z
 #pragma unroll
             for (int k = 0; k < K; ++k)
 #pragma unroll
                 for (int c = 0; c < CH; ++c) {
-                    before[k][c] = begin[c];
+                    e1[k][c] = LRU ? e1[k][c] - begin[c] : begin[c] - e1[k][c];
                     begin[c] = fmaf(a[k][c], begin[c], v[k][c]);
+                    if (HASZ) zz[k][c] *= begin[c];
                 }
-            char *to_x = static_cast<char *>(p.dx) + at * p.dx_stride * Ln::ES, *to_f = static_cast<char *>(p.df) + at * p.df_stride * Ln::ES;
-            char *to_i = static_cast<char *>(p.di) + at * p.di_stride * Ln::ES, *to_z = static_cast<char *>(p.dz) + at * p.dz_stride * Ln::ES;
+            if (HASZ && p.dz) wdz.template store<TAIL>(zz, t0 + wave0, run, len, ln);
 #pragma unroll
-            for (int k = K - 1; k >= 0; --k) {
-                if (t + k >= len) continue;
-                float f[CH], x[CH], i[CH], z[CH], dy[CH], dx[CH], df[CH], di[CH], dz[CH];
-                Ln::decode(rf[k], f);
-                Ln::decode(rx[k], x);
-                if (p.i) Ln::decode(ri[k], i);
-                if (p.z) {
-                    Ln::decode(rz[k], z);
-                    Ln::decode(ry[k], dy);
-                }
+            for (int k = K - 1; k >= 0; --k)
 #pragma unroll
                 for (int c = 0; c < CH; ++c) {
-                    const float Gt = g[k][c] + flow[c], at_k = a[k][c], w = v[k][c];
-                    flow[c] = at_k * Gt;
-                    if (p.z) {
-                        const float s = sigmoid(z[c]), h = fmaf(at_k, before[k][c], w);
-                        dz[c] = dy[c] * h * s * fmaf(z[c], 1.f - s, 1.f);
+                    const float G = g[k][c] + flow[c];
+                    flow[c] = a[k][c] * G;
+                    ex[k][c] *= G;
+                    if (HASI) {
+                        ei[k][c] *= G;
+                        sumI[c] += ei[k][c];
                     }
-                    float si = 1.f, ni = 0.f;
-                    if (p.i) sigmoids(i[c] + ib[c], si, ni);
-                    float r, nr, m;
-                    sigmoids(f[c] + fb[c], r, nr);
-                    if constexpr (LRU) {
-                        const float q = rate[c] * r, m2 = one_minus_square(q, at_k);
-                        m = __builtin_amdgcn_sqrtf(m2);
-                        const float s = -kLn2 * q;
-                        const float E = (s * at_k) * Gt * fmaf(w * at_k, __builtin_amdgcn_rcpf(fmaxf(m2, 1e-37f)), -before[k][c]);
-                        sumA[c] += E;
-                        df[c] = E * nr;
-                    } else {
-                        m = nr;
-                        df[c] = Gt * (r * nr) * (before[k][c] - si * x[c]);
+                    e0[k][c] *= G * e1[k][c];
+                    if (LRU) {
+                        sumA[c] += e0[k][c];
+                        e0[k][c] *= e2[k][c];
                     }
-                    sumF[c] += df[c];
-                    dx[c] = Gt * m * si;
-                    if (p.i) {
-                        di[c] = Gt * w * ni;
-                        sumI[c] += di[c];
-                    }
+                    sumF[c] += e0[k][c];
                 }
-                if (p.dx) Ln::store(to_x + k * p.dx_stride * Ln::ES, odx, live, dx);
-                if (p.df) Ln::store(to_f + k * p.df_stride * Ln::ES, odf, live, df);
-                if (p.di) Ln::store(to_i + k * p.di_stride * Ln::ES, odi, live, di);
-                if (p.dz) Ln::store(to_z + k * p.dz_stride * Ln::ES, odz, live, dz);
-            }
+            if (p.dx) wdx.template store<TAIL>(ex, t0 + wave0, run, len, ln);
+            if (p.df) wdf.template store<TAIL>(e0, t0 + wave0, run, len, ln);
+            if (HASI && p.di) wdi.template store<TAIL>(ei, t0 + wave0, run, len, ln);
+            wdx.move(-T);
+            wdf.move(-T);
+            wdi.move(-T);
+            wdz.move(-T);
+        }
+    };
+    const std::true_type tail{};
+    const std::false_type full{};
+    int buf = 0;
+    for (; t0 >= from + whole; t0 -= T, buf ^= 1) {
+        fetch_tail(t0);
+        tile(tail, t0, buf, [] {});
+    }
+    if (whole > 0) {
+        prefetch(t0);
+        // behind a tile's loads a wave issues the stores of the tile before it; how many is known where every lane of the workgroup stores and all gradients are wanted
+        const bool known = first + Ln::CW <= p.C && p.dx && p.df && (!HASI || p.di) && (!HASZ || p.dz);
+        bool stored = false;
+        for (; t0 >= from; t0 -= T, buf ^= 1) {
+            if (OUT && known && stored) wait_but<K * (2 + HASI + HASZ)>();
+            else wait_but<0>();
+            each([&](auto &, uint32_t (&r)[K], int i) {
+#pragma unroll
+                for (int k = 0; k < K; ++k) r[k] = ahead[i][k][wave][lane];
+            });
+            tile(full, t0, buf, [&] {
+                if (t0 > from) {
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // what is there has been read
+                    prefetch(t0 - T);
+                }
+            });
+            stored = true;
         }
     }
     if constexpr (!OUT) {
-        if (wave != 0 || grp != 0) return;
-        store_channels<CH>(p.seg_r + seg0 + (size_t)seg * p.C, live, carry);
-        store_channels<CH>(p.seg_p + seg0 + (size_t)seg * p.C, live, prod);
+        if (wave != 0 || run != 0) return;
+        ln.put_floats(p.seg_r + seg0 + (size_t)seg * p.C, carry);
+        ln.put_floats(p.seg_p + seg0 + (size_t)seg * p.C, prod);
     } else {
-        if (seg == 0 && p.dh_in && wave == 0 && grp == 0) store_channels<CH>(p.dh_in + (size_t)b * p.C + c0, live, carry);
+        if (seg == 0 && p.dh_in && wave == 0 && run == 0) ln.put_floats(p.dh_in + (size_t)b * p.C, carry);
         if (!p.partial) return;
         __syncthreads();                                            // the last tile's pairs have been read
+        float sums[3][CH];
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
+            sums[0][c] = sumA[c];
+            sums[1][c] = sumF[c];
+            sums[2][c] = sumI[c];
 #pragma unroll
-            for (int d = CL; d < 64; d *= 2) {
-                sumA[c] += __shfl_xor(sumA[c], d);
-                sumF[c] += __shfl_xor(sumF[c], d);
-                sumI[c] += __shfl_xor(sumI[c], d);
-            }
-        }
-        if (grp == 0) {
-#pragma unroll
-            for (int c = 0; c < CH; ++c) {
-                pairs[0][wave][cl][c] = sumA[c];
-                pairs[0][wave][cl][CH + c] = sumF[c];
-                pairs[0][wave][cl][2 * CH + c] = sumI[c];
+            for (int k = 0; k < 3; ++k) {
+                sums[k][c] += __shfl_xor(sums[k][c], 16);
+                sums[k][c] += __shfl_xor(sums[k][c], 32);
+                if (run == 0) pairs[0][wave][cl][k * CH + c] = sums[k][c];
             }
         }
         __syncthreads();
-        if (wave >= 3 || grp != 0) return;                          // wave k adds the k-th vector's
+        if (wave >= 3 || run != 0) return;                          // wave k adds the k-th vector's
         float s[CH];
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             s[c] = 0.f;
             for (int w = 0; w < W; ++w) s[c] += pairs[0][w][cl][wave * CH + c];
         }
-        store_channels<CH>(p.partial + (((size_t)b * p.seg_count + seg) * 3 + wave) * p.C + c0, live, s);
+        ln.put_floats(p.partial + (((size_t)b * p.seg_count + seg) * 3 + wave) * p.C, s);
     }
 }
 
-template <int IO, int CL, bool LRU>
+template <int IO, int W, bool LRU, bool HASI, bool HASZ>
 int launch(const GatedGradParams &p, hipStream_t stream)
 {
-    constexpr int CW = GatedLane<IO, CL>::CW;
+    constexpr int CW = GatedLane<IO>::CW;
     const unsigned groups = (unsigned)((p.C + CW - 1) / CW);
-    const dim3 block(64 * kGatedWaves);
+    const dim3 block(64 * W);
     if (p.seg_count > 1) {
-        hipLaunchKernelGGL((gated_backward_kernel<IO, CL, LRU, false>), dim3(groups, p.seg_count - 1, p.batch), block, 0, stream, p);
+        hipLaunchKernelGGL((gated_backward_kernel<IO, W, LRU, false, HASZ, false>), dim3(groups, p.seg_count - 1, p.batch), block, 0, stream, p);
         const int e = (int)hipGetLastError();
         if (e != 0) return e;
     }
-    hipLaunchKernelGGL((gated_backward_kernel<IO, CL, LRU, true>), dim3(groups, p.seg_count, p.batch), block, 0, stream, p);
+    hipLaunchKernelGGL((gated_backward_kernel<IO, W, LRU, HASI, HASZ, true>), dim3(groups, p.seg_count, p.batch), block, 0, stream, p);
     return (int)hipGetLastError();
 }
 
-template <int IO, bool LRU>
-int launch_lanes(const GatedGradParams &p, hipStream_t stream)
+template <int IO, int W, bool LRU>
+int launch_gates(const GatedGradParams &p, hipStream_t stream)
 {
-    switch (p.lanes) {
-        case 64: return launch<IO, 64, LRU>(p, stream);
-        case 32: return launch<IO, 32, LRU>(p, stream);
-        case 16: return launch<IO, 16, LRU>(p, stream);
-        case 8: return launch<IO, 8, LRU>(p, stream);
-    }
-    return (int)hipErrorInvalidValue;
+    if (p.i) return p.z ? launch<IO, W, LRU, true, true>(p, stream) : launch<IO, W, LRU, true, false>(p, stream);
+    return p.z ? launch<IO, W, LRU, false, true>(p, stream) : launch<IO, W, LRU, false, false>(p, stream);
+}
+
+template <int IO, bool LRU>
+int launch_waves(const GatedGradParams &p, hipStream_t stream)
+{
+    return p.waves == 4 ? launch_gates<IO, 4, LRU>(p, stream) : launch_gates<IO, 8, LRU>(p, stream);
 }
 
 }  // namespace
@@ -304,8 +341,8 @@ int launch_lanes(const GatedGradParams &p, hipStream_t stream)
 int launch_gated_backward(const GatedGradParams &p, hipStream_t stream)
 {
     int e;
-    if (p.io == SSMV_BF16) e = p.lru ? launch_lanes<SSMV_BF16, true>(p, stream) : launch_lanes<SSMV_BF16, false>(p, stream);
-    else e = p.lru ? launch_lanes<SSMV_F32, true>(p, stream) : launch_lanes<SSMV_F32, false>(p, stream);
+    if (p.io == SSMV_BF16) e = p.lru ? launch_waves<SSMV_BF16, true>(p, stream) : launch_waves<SSMV_BF16, false>(p, stream);
+    else e = p.lru ? launch_waves<SSMV_F32, true>(p, stream) : launch_waves<SSMV_F32, false>(p, stream);
     if (e != 0 || !p.partial) return e;
     const ColumnSums to{{p.dA, p.df_bias, p.di_bias}, {p.A, nullptr, nullptr}};
     return launch_column_sums(p.partial, p.batch * p.seg_count, p.C, to, stream);

@@ -1,4 +1,6 @@
 // The gated linear recurrence over a sequence, from state to state, and over one token of every row.
+#include <type_traits>
+
 #include "gated_common.h"
 
 namespace ssmv {
@@ -17,140 +19,116 @@ __device__ __forceinline__ void coefficients(float f, float rate, float &a, floa
     }
 }
 
-// h <- a h + v: a run of tokens is the pair (product of a, state that it leaves from zero), and pairs combine in order.  A lane forms the pair of its run, the lanes of a
-// wave and then the waves of the workgroup combine theirs (LDS, one barrier a tile), and every lane goes through its run again from the state that it starts from.  So a
-// token is read once; the gates stay in registers between the two walks.
+// h <- a h + v: a run of tokens is the pair (product of a, state that it leaves from zero), and pairs combine in order.  A lane forms the pair of its run, the runs of a
+// wave (permutes) and then the waves of the workgroup combine theirs (LDS, one barrier a tile), and every lane goes through its run again from the state that it starts from.  So a
+// token is read once; the gates stay in registers between the two walks, and the next tile's values are on their way.
 // OUT false: only the pairs of whole segments, of all but the last.
-template <int IO, int CL, bool LRU, bool OUT>
-__global__ __launch_bounds__(64 * kGatedWaves) void gated_recurrence_kernel(const GatedParams p)
+template <int IO, int W, bool LRU, bool HASI, bool HASZ, bool OUT>
+__global__ __launch_bounds__(64 * W) void gated_recurrence_kernel(const GatedParams p)
 {
-    using Ln = GatedLane<IO, CL>;
-    constexpr int CH = Ln::CH, G = Ln::G, T = Ln::T, K = kGatedRun, W = kGatedWaves;
-    __shared__ __attribute__((aligned(16))) float pairs[2][W][CL][2 * CH];
-    const unsigned lane = threadIdx.x & 63u, cl = lane % CL, grp = lane / CL;
+    using Ln = GatedLane<IO>;
+    constexpr int CH = Ln::CH, T = W * kWaveTokens;
+    __shared__ __attribute__((aligned(16))) float pairs[2][W][kLanes][2 * CH];
+    const unsigned lane = threadIdx.x & 63u, cl = lane % kLanes, run = lane / kLanes;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int c0 = (int)xcd_contiguous(blockIdx.x, gridDim.x) * Ln::CW + (int)cl * CH, live = min(max(p.C - c0, 0), CH), seg = blockIdx.y;
+    const int first = (int)xcd_contiguous(blockIdx.x, gridDim.x) * Ln::CW, seg = blockIdx.y;
+    const Ln ln(first + (int)cl * CH, p.C);
     int b = blockIdx.z;
-    if (p.seq_len && p.batch > 1 && p.batch <= 64) b = zth_longest(p.seq_len, p.batch, b, lane);
+    if (p.seq_len && p.batch > 1 && p.batch <= 64) b = __builtin_amdgcn_readfirstlane(zth_longest(p.seq_len, p.batch, b, lane));
     const int all = p.seq_len ? min(max(p.seq_len[b], 0), p.L) : p.L;
     const int from = seg * p.seg_len, len = min(all, from + p.seg_len);
     const bool last = len == all;
     if (seg > 0 && (OUT ? from >= all : last)) return;
-    const size_t seg0 = (size_t)b * p.seg_count * p.C + c0;
+    const size_t seg0 = (size_t)b * p.seg_count * p.C;
 
     float h[CH], prod[CH], rate[CH], fb[CH], ib[CH];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        h[c] = 0.f;
+        h[c] = rate[c] = fb[c] = ib[c] = 0.f;
         prod[c] = 1.f;
-        rate[c] = LRU && c < live ? decay_exponent(p.A[c0 + c]) : 0.f;
-        fb[c] = p.f_bias && c < live ? p.f_bias[c0 + c] : 0.f;
-        ib[c] = p.i_bias && c < live ? p.i_bias[c0 + c] : 0.f;
     }
+    if (LRU) {
+        ln.floats(p.A, rate);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) rate[c] = decay_exponent(rate[c]);
+    }
+    if (p.f_bias) ln.floats(p.f_bias, fb);
+    if (HASI && p.i_bias) ln.floats(p.i_bias, ib);
     if (seg == 0) {
         const int src = p.src_row ? p.src_row[b] : b;
-        if (OUT && p.seg_count > 1) load_channels<CH>(p.seg_h + seg0 + (size_t)(p.seg_count - 1) * p.C, live, h);    // h_out may be h_in, and its writer another workgroup
-        else if (p.h_in && (unsigned)src < (unsigned)p.rows_in) load_channels<CH>(p.h_in + (size_t)src * p.C + c0, live, h);
-        if (!OUT && wave == 0 && grp == 0) store_channels<CH>(p.seg_h + seg0 + (size_t)(p.seg_count - 1) * p.C, live, h);
+        if (OUT && p.seg_count > 1) ln.floats(p.seg_h + seg0 + (size_t)(p.seg_count - 1) * p.C, h);    // h_out may be h_in, and its writer another workgroup
+        else if (p.h_in && (unsigned)src < (unsigned)p.rows_in) ln.floats(p.h_in + (size_t)src * p.C, h);
+        if (!OUT && wave == 0 && run == 0) ln.put_floats(p.seg_h + seg0 + (size_t)(p.seg_count - 1) * p.C, h);
         if (!OUT && last) return;
     } else if (OUT) {
-        load_channels<CH>(p.seg_h + seg0, live, h);
+        ln.floats(p.seg_h + seg0, h);
         for (int j = 1; j < seg; ++j) {
             float sp[CH], sh[CH];
-            load_channels<CH>(p.seg_p + seg0 + (size_t)j * p.C, live, sp);
-            load_channels<CH>(p.seg_h + seg0 + (size_t)j * p.C, live, sh);
+            ln.floats(p.seg_p + seg0 + (size_t)j * p.C, sp);
+            ln.floats(p.seg_h + seg0 + (size_t)j * p.C, sh);
 #pragma unroll
             for (int c = 0; c < CH; ++c) h[c] = fmaf(sp[c], h[c], sh[c]);
         }
     }
 
-    const size_t tok0 = (size_t)b * p.L;
-    const int run0 = (wave * G + (int)grp) * K;                     // the lane's tokens in a tile
-    auto offset = [&](size_t stride) { return (unsigned)((grp * K * (unsigned)stride + (unsigned)c0) * Ln::ES); };
-    const unsigned ox = offset(p.x_stride), of = offset(p.f_stride), oi = offset(p.i_stride), oz = offset(p.z_stride), oy = offset(p.y_stride);
-    uint32_t rx[K], rf[K], ri[K], rz[K];
-    auto fetch = [&](int t0) {
-        const size_t at = tok0 + t0 + wave * G * K;
-        Ln::load_run(rx, p.x, p.x_stride, at, ox, live, t0 + run0, len);
-        Ln::load_run(rf, p.f, p.f_stride, at, of, live, t0 + run0, len);
-        if (p.i) Ln::load_run(ri, p.i, p.i_stride, at, oi, live, t0 + run0, len);
-        if (OUT && p.z) Ln::load_run(rz, p.z, p.z_stride, at, oz, live, t0 + run0, len);
+    const int wave0 = wave * kWaveTokens, run0 = wave0 + (int)run * kRun;       // the wave's and the lane's tokens in a tile
+    const size_t tok0 = (size_t)b * p.L + from + wave0;
+    Walk<IO> wx(p.x, p.x_stride, tok0, run, ln), wf(p.f, p.f_stride, tok0, run, ln), wi(p.i, p.i_stride, tok0, run, ln), wz(p.z, p.z_stride, tok0, run, ln),
+        wy(p.y, p.y_stride, tok0, run, ln);
+    const int whole = p.C >= CH ? len - from - (len - from) % T : 0;             // tokens in whole tiles; a row of one bf16 channel takes the other path, too
+    uint32_t rx[kRun], rf[kRun], ri[kRun], rz[kRun];
+    auto fetch = [&](auto tail, int t0) {                           // and on to the next tile
+        auto one = [&](auto &w, uint32_t (&r)[kRun]) {
+            if constexpr (decltype(tail)::value) w.load_tail(r, t0 + wave0, run, len, ln);
+            else w.load(r);
+            w.move(T);
+        };
+        one(wf, rf);
+        one(wx, rx);
+        if (HASI) one(wi, ri);
+        if (OUT && HASZ) one(wz, rz);
     };
-    if (from < len) fetch(from);
-    for (int t0 = from, buf = 0; t0 < len; t0 += T, buf ^= 1) {
+    auto tile = [&](auto tail, int t0, int buf, auto &&next) {
+        constexpr bool TAIL = decltype(tail)::value;
         const int t = t0 + run0;
-        float a[K][CH], v[K][CH], gate[OUT ? K : 1][CH];
+        float a[kRun][CH], v[kRun][CH], y[OUT ? kRun : 1][CH];
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            float f[CH], x[CH];
+        for (int k = 0; k < kRun; ++k) {
+            float f[CH], x[CH], i[CH], z[CH];
             Ln::decode(rf[k], f);
             Ln::decode(rx[k], x);
+            if (HASI) Ln::decode(ri[k], i);
+            if (OUT && HASZ) Ln::decode(rz[k], z);
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 float m;
                 coefficients<LRU>(f[c] + fb[c], rate[c], a[k][c], m);
                 v[k][c] = m * x[c];
-            }
-        }
-        if (p.i) {
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                float g[CH];
-                Ln::decode(ri[k], g);
-#pragma unroll
-                for (int c = 0; c < CH; ++c) v[k][c] *= sigmoid(g[c] + ib[c]);
-            }
-        }
-        if (OUT && p.z) {
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                float z[CH];
-                Ln::decode(rz[k], z);
-#pragma unroll
-                for (int c = 0; c < CH; ++c) gate[OUT ? k : 0][c] = z[c] * sigmoid(z[c]);
-            }
-        }
-        if (t + K > len) {                                          // tokens that are none leave the state as it is
-#pragma unroll
-            for (int k = 0; k < K; ++k)
-#pragma unroll
-                for (int c = 0; c < CH; ++c) {
+                if (HASI) v[k][c] *= sigmoid(i[c] + ib[c]);
+                if (OUT) y[OUT ? k : 0][c] = HASZ ? z[c] * sigmoid(z[c]) : 1.f;
+                if (TAIL) {                                         // tokens that are none leave the state as it is
                     a[k][c] = t + k < len ? a[k][c] : 1.f;
                     v[k][c] = t + k < len ? v[k][c] : 0.f;
                 }
+            }
         }
-        if (t0 + T < len) fetch(t0 + T);
-        float P[CH], H[CH], Pe[CH], He[CH];
+        next();
+        float Pe[CH], He[CH], Pt[CH], Ht[CH];
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            P[c] = a[0][c];
-            H[c] = v[0][c];
+            float P = a[0][c], H = v[0][c];
 #pragma unroll
-            for (int k = 1; k < K; ++k) {
-                P[c] *= a[k][c];
-                H[c] = fmaf(a[k][c], H[c], v[k][c]);
+            for (int k = 1; k < kRun; ++k) {
+                P *= a[k][c];
+                H = fmaf(a[k][c], H, v[k][c]);
             }
-            Pe[c] = 1.f;
-            He[c] = 0.f;
-            if constexpr (G > 1) {
-#pragma unroll
-                for (int d = CL; d < 64; d *= 2) {
-                    const float p1 = __shfl_up(P[c], d), h1 = __shfl_up(H[c], d);
-                    if ((int)lane >= d) {
-                        H[c] = fmaf(P[c], h1, H[c]);
-                        P[c] *= p1;
-                    }
-                }
-                const float p1 = __shfl_up(P[c], CL), h1 = __shfl_up(H[c], CL);
-                Pe[c] = grp > 0 ? p1 : 1.f;
-                He[c] = grp > 0 ? h1 : 0.f;
-            }
+            combine_forward(P, H, run, Pe[c], He[c], Pt[c], Ht[c]);
         }
-        if (grp == G - 1) {
+        if (run == 0) {
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                pairs[buf][wave][cl][c] = P[c];
-                pairs[buf][wave][cl][CH + c] = H[c];
+                pairs[buf][wave][cl][c] = Pt[c];
+                pairs[buf][wave][cl][CH + c] = Ht[c];
             }
         }
         __syncthreads();
@@ -159,7 +137,7 @@ __global__ __launch_bounds__(64 * kGatedWaves) void gated_recurrence_kernel(cons
         for (int w = 0; w < W; ++w) {
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                if (w == wave) start[c] = h[c];
+                start[c] = w == wave ? h[c] : w == 0 ? 0.f : start[c];
                 const float pw = pairs[buf][w][cl][c];
                 h[c] = fmaf(pw, h[c], pairs[buf][w][cl][CH + c]);
                 if (!OUT) prod[c] *= pw;
@@ -169,27 +147,38 @@ __global__ __launch_bounds__(64 * kGatedWaves) void gated_recurrence_kernel(cons
 #pragma unroll
             for (int c = 0; c < CH; ++c) start[c] = fmaf(Pe[c], start[c], He[c]);
             if (p.states && t % SSMV_GATED_TILE == 0 && t < len)
-                store_channels<CH>(p.states + ((size_t)b * ((p.L + SSMV_GATED_TILE - 1) / SSMV_GATED_TILE) + t / SSMV_GATED_TILE) * p.C + c0, live, start);
-            char *row = static_cast<char *>(p.y) + (tok0 + t0 + wave * G * K) * p.y_stride * Ln::ES;
+                ln.put_floats(p.states + ((size_t)b * ((p.L + SSMV_GATED_TILE - 1) / SSMV_GATED_TILE) + t / SSMV_GATED_TILE) * p.C, start);
 #pragma unroll
-            for (int k = 0; k < K; ++k) {
-                float y[CH];
+            for (int k = 0; k < kRun; ++k)
 #pragma unroll
                 for (int c = 0; c < CH; ++c) {
                     start[c] = fmaf(a[k][c], start[c], v[k][c]);
-                    y[c] = p.z ? start[c] * gate[k][c] : start[c];
+                    y[k][c] = HASZ ? start[c] * y[k][c] : start[c];
                 }
-                if (t + k < len) Ln::store(row + k * p.y_stride * Ln::ES, oy, live, y);
-            }
+            wy.template store<TAIL>(y, t0 + wave0, run, len, ln);
+            wy.move(T);
         }
+    };
+    // whole tiles, the next one on its way, then the rest
+    const std::true_type tail{};
+    const std::false_type full{};
+    int t0 = from, buf = 0;
+    if (whole > 0) {
+        fetch(full, from);
+        for (; t0 < from + whole; t0 += T, buf ^= 1)
+            tile(full, t0, buf, [&] { if (t0 + T < from + whole) fetch(full, t0 + T); });
     }
-    if (wave != 0 || grp != 0) return;
+    for (; t0 < len; t0 += T, buf ^= 1) {                           // once, but for a row of one bf16 channel
+        fetch(tail, t0);
+        tile(tail, t0, buf, [] {});
+    }
+    if (wave != 0 || run != 0) return;
     if constexpr (OUT) {
-        if (last && p.h_out) store_channels<CH>(p.h_out + (size_t)b * p.C + c0, live, h);
-        if (all == 0 && p.states) store_channels<CH>(p.states + (size_t)b * ((p.L + SSMV_GATED_TILE - 1) / SSMV_GATED_TILE) * p.C + c0, live, h);
+        if (last && p.h_out) ln.put_floats(p.h_out + (size_t)b * p.C, h);
+        if (all == 0 && p.states) ln.put_floats(p.states + (size_t)b * ((p.L + SSMV_GATED_TILE - 1) / SSMV_GATED_TILE) * p.C, h);
     } else {
-        store_channels<CH>(p.seg_h + seg0 + (size_t)seg * p.C, live, h);
-        store_channels<CH>(p.seg_p + seg0 + (size_t)seg * p.C, live, prod);
+        ln.put_floats(p.seg_h + seg0 + (size_t)seg * p.C, h);
+        ln.put_floats(p.seg_p + seg0 + (size_t)seg * p.C, prod);
     }
 }
 
@@ -197,26 +186,29 @@ __global__ __launch_bounds__(64 * kGatedWaves) void gated_recurrence_kernel(cons
 template <int IO, bool LRU>
 __global__ __launch_bounds__(256) void gated_token_kernel(const GatedParams p)
 {
-    using Ln = GatedLane<IO, 64>;
+    using Ln = GatedLane<IO>;
     constexpr int CH = Ln::CH;
-    const int c0 = ((int)blockIdx.x * 256 + (int)threadIdx.x) * CH, live = min(max(p.C - c0, 0), CH), b = blockIdx.y;
-    if (live == 0) return;
+    const int b = blockIdx.y;
+    const Ln ln(((int)blockIdx.x * 256 + (int)threadIdx.x) * CH, p.C);
+    if (ln.skip >= CH || !ln.mine(CH - 1) && !ln.mine(0)) return;
     const bool none = p.seq_len && p.seq_len[b] <= 0;
     const int src = p.src_row ? p.src_row[b] : b;
-    auto at = [&](const void *t, size_t stride) { return static_cast<const char *>(t) + (size_t)b * stride * Ln::ES; };
-    const unsigned off = (unsigned)c0 * Ln::ES;
-    float h[CH], x[CH], f[CH], i[CH], z[CH];
+    auto row = [&](const void *t, size_t stride) { return static_cast<const char *>(t) + (size_t)b * stride * Ln::ES; };
+    float h[CH], x[CH], f[CH], i[CH], z[CH], rate[CH], fb[CH], ib[CH];
     uint32_t rx = 0, rf = 0, ri = 0, rz = 0;
     if (!none) {
-        rx = Ln::load(at(p.x, p.x_stride), off, live);
-        rf = Ln::load(at(p.f, p.f_stride), off, live);
-        if (p.i) ri = Ln::load(at(p.i, p.i_stride), off, live);
-        if (p.z) rz = Ln::load(at(p.z, p.z_stride), off, live);
+        rx = ln.load_any(row(p.x, p.x_stride));
+        rf = ln.load_any(row(p.f, p.f_stride));
+        if (p.i) ri = ln.load_any(row(p.i, p.i_stride));
+        if (p.z) rz = ln.load_any(row(p.z, p.z_stride));
     }
 #pragma unroll
-    for (int c = 0; c < CH; ++c) h[c] = 0.f;
-    if (p.h_in && (unsigned)src < (unsigned)p.rows_in) load_channels<CH>(p.h_in + (size_t)src * p.C + c0, live, h);
-    if (p.states) store_channels<CH>(p.states + (size_t)b * p.C + c0, live, h);
+    for (int c = 0; c < CH; ++c) h[c] = rate[c] = fb[c] = ib[c] = 0.f;
+    if (p.h_in && (unsigned)src < (unsigned)p.rows_in) ln.floats(p.h_in + (size_t)src * p.C, h);
+    if (LRU) ln.floats(p.A, rate);
+    if (p.f_bias) ln.floats(p.f_bias, fb);
+    if (p.i_bias) ln.floats(p.i_bias, ib);
+    if (p.states) ln.put_floats(p.states + (size_t)b * p.C, h);
     Ln::decode(rx, x);
     Ln::decode(rf, f);
     Ln::decode(ri, i);
@@ -224,56 +216,56 @@ __global__ __launch_bounds__(256) void gated_token_kernel(const GatedParams p)
     float y[CH];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        const int ch = min(c0 + c, p.C - 1);
         float a, m;
-        coefficients<LRU>(f[c] + (p.f_bias ? p.f_bias[ch] : 0.f), LRU ? decay_exponent(p.A[ch]) : 0.f, a, m);
+        coefficients<LRU>(f[c] + fb[c], LRU ? decay_exponent(rate[c]) : 0.f, a, m);
         float v = m * x[c];
-        if (p.i) v *= sigmoid(i[c] + (p.i_bias ? p.i_bias[ch] : 0.f));
+        if (p.i) v *= sigmoid(i[c] + ib[c]);
         if (!none) h[c] = fmaf(a, h[c], v);
         y[c] = p.z ? h[c] * (z[c] * sigmoid(z[c])) : h[c];
     }
-    if (!none) Ln::store(const_cast<char *>(at(p.y, p.y_stride)), off, live, y);
-    if (p.h_out) store_channels<CH>(p.h_out + (size_t)b * p.C + c0, live, h);
+    if (!none) ln.store_any(const_cast<char *>(row(p.y, p.y_stride)), y);
+    if (p.h_out) ln.put_floats(p.h_out + (size_t)b * p.C, h);
 }
 
-template <int IO, int CL, bool LRU>
+template <int IO, int W, bool LRU, bool HASI, bool HASZ>
 int launch(const GatedParams &p, hipStream_t stream)
 {
-    constexpr int CW = GatedLane<IO, CL>::CW;
+    constexpr int CW = GatedLane<IO>::CW;
     const unsigned groups = (unsigned)((p.C + CW - 1) / CW);
-    const dim3 block(64 * kGatedWaves);
+    const dim3 block(64 * W);
     if (p.seg_count > 1) {
-        hipLaunchKernelGGL((gated_recurrence_kernel<IO, CL, LRU, false>), dim3(groups, p.seg_count - 1, p.batch), block, 0, stream, p);
+        hipLaunchKernelGGL((gated_recurrence_kernel<IO, W, LRU, HASI, false, false>), dim3(groups, p.seg_count - 1, p.batch), block, 0, stream, p);
         const int e = (int)hipGetLastError();
         if (e != 0) return e;
     }
-    hipLaunchKernelGGL((gated_recurrence_kernel<IO, CL, LRU, true>), dim3(groups, p.seg_count, p.batch), block, 0, stream, p);
+    hipLaunchKernelGGL((gated_recurrence_kernel<IO, W, LRU, HASI, HASZ, true>), dim3(groups, p.seg_count, p.batch), block, 0, stream, p);
     return (int)hipGetLastError();
 }
 
+template <int IO, int W, bool LRU>
+int launch_gates(const GatedParams &p, hipStream_t stream)
+{
+    if (p.i) return p.z ? launch<IO, W, LRU, true, true>(p, stream) : launch<IO, W, LRU, true, false>(p, stream);
+    return p.z ? launch<IO, W, LRU, false, true>(p, stream) : launch<IO, W, LRU, false, false>(p, stream);
+}
+
 template <int IO, bool LRU>
-int launch_lanes(const GatedParams &p, hipStream_t stream)
+int launch_waves(const GatedParams &p, hipStream_t stream)
 {
     if (p.L == 1) {
-        constexpr int per = 256 * GatedLane<IO, 64>::CH;
+        constexpr int per = 256 * GatedLane<IO>::CH;
         hipLaunchKernelGGL((gated_token_kernel<IO, LRU>), dim3((p.C + per - 1) / per, p.batch), dim3(256), 0, stream, p);
         return (int)hipGetLastError();
     }
-    switch (p.lanes) {
-        case 64: return launch<IO, 64, LRU>(p, stream);
-        case 32: return launch<IO, 32, LRU>(p, stream);
-        case 16: return launch<IO, 16, LRU>(p, stream);
-        case 8: return launch<IO, 8, LRU>(p, stream);
-    }
-    return (int)hipErrorInvalidValue;
+    return p.waves == 4 ? launch_gates<IO, 4, LRU>(p, stream) : launch_gates<IO, 16, LRU>(p, stream);
 }
 
 }  // namespace
 
 int launch_gated_recurrence(const GatedParams &p, hipStream_t stream)
 {
-    if (p.io == SSMV_BF16) return p.lru ? launch_lanes<SSMV_BF16, true>(p, stream) : launch_lanes<SSMV_BF16, false>(p, stream);
-    return p.lru ? launch_lanes<SSMV_F32, true>(p, stream) : launch_lanes<SSMV_F32, false>(p, stream);
+    if (p.io == SSMV_BF16) return p.lru ? launch_waves<SSMV_BF16, true>(p, stream) : launch_waves<SSMV_BF16, false>(p, stream);
+    return p.lru ? launch_waves<SSMV_F32, true>(p, stream) : launch_waves<SSMV_F32, false>(p, stream);
 }
 
 }  // namespace ssmv

@@ -36,8 +36,7 @@ struct GatedParams {
     float *h_out, *states;
     size_t x_stride, f_stride, i_stride, z_stride, y_stride;
     int batch, rows_in, C, L, io, lru;
-    int lanes;               // channel lanes of a wave: see GatedPlan
-    int seg_len, seg_count;
+    int waves, seg_len, seg_count;       // see GatedPlan
     float *seg_p;            // [batch][seg_count][C] products of the segments' decays
     float *seg_h;            // [batch][seg_count][C] end states of the segments from zero (the first one's from its start); last place: the start state
 };
@@ -50,7 +49,7 @@ struct GatedGradParams {
     float *dA, *df_bias, *di_bias, *dh_in;
     size_t x_stride, f_stride, i_stride, z_stride, dy_stride, dx_stride, df_stride, di_stride, dz_stride;
     int batch, C, L, io, lru;
-    int lanes, seg_len, seg_count;
+    int waves, seg_len, seg_count;
     float *seg_p;            // [batch][seg_count][C] products of the segments' decays
     float *seg_r;            // [batch][seg_count][C] what flows out of a segment's front when nothing flows into its end
     float *partial;          // [batch][seg_count][3][C] sums for A, f_bias, i_bias of a segment's tokens; NULL: none is wanted
@@ -87,21 +86,21 @@ int launch_column_sums(const float *partial, int parts, int C, const ColumnSums 
 constexpr int kNormParts = 512;
 inline int norm_parts(int rows) { return rows < kNormParts ? rows : kNormParts; }
 
-// How the recurrence is laid on the chip.  A workgroup takes 512 threads; `lanes` lanes of a wave lie side by side over the channels (two bf16
-// channels a lane, or one fp32), the others over the tokens, 8 a lane: 64 * 64 / lanes tokens a tile.
+// How the recurrence is laid on the chip.  16 lanes of a wave lie side by side over the channels (two bf16 channels a lane, or one fp32), the wave's four rows of lanes and
+// the workgroup's waves over the tokens, 4 a lane: 16 tokens a wave and tile.
 struct GatedPlan {
-    int lanes;               // 64, 32, 16, 8
+    int waves;               // of a workgroup: 4, or 16 (forward) or 8 (backward, which needs more registers)
     int seg_len, seg_count;  // tokens of a segment (whole tiles), segments of the longest sequence
 };
-inline GatedPlan gated_plan(int batch, int C, int L)
+inline GatedPlan gated_plan(int batch, int C, int L, bool backward)
 {
     // counted in fp32 lanes, so that the plan, and with it the workspace, does not depend on the type
-    GatedPlan r{64, L, 1};
-    auto groups = [&](int lanes) { return (long)batch * ((C + lanes - 1) / lanes); };
-    while (r.lanes > 8 && groups(r.lanes) < 512 && L > 4096 / r.lanes) r.lanes /= 2;
-    const int tile = 4096 / r.lanes, tiles = (L + tile - 1) / tile;
+    const long groups = (long)batch * ((C + 15) / 16);
+    GatedPlan r{4, L, 1};
+    if (groups < 1024 && L > 64) r.waves = backward ? 8 : 16;
+    const int tile = 16 * r.waves, tiles = (L + tile - 1) / tile;
     int want = 1;
-    while (want < 16 && groups(r.lanes) * want < 256 && tiles >= 8 * want) want *= 2;
+    while (want < 32 && groups * want < 256 && tiles >= 4 * want) want *= 2;
     if (want > 1) {
         r.seg_len = (tiles + want - 1) / want * tile;
         r.seg_count = (L + r.seg_len - 1) / r.seg_len;
@@ -165,18 +164,15 @@ __device__ __forceinline__ float decay_exponent(float A)
     return a < -3.402823466e+38f ? -3.402823466e+38f : a;
 }
 
-// 1 - a^2 for a = 2^q, q <= 0: near a = 1, where the difference loses it, -expm1(u) at u = 2 q ln 2 by its series
-// -u (1 + u/2 + u^2/6 + ... + u^6/5040), off by less than 2e-8 for |u| < 0.35; elsewhere a^2 is at most 0.71 and its roundings count 2.4 times.
+// 1 - a^2 for a = 2^q, q <= 0.  Near a = 1, where the difference loses it, -expm1(u) at u = 2 q ln 2, |u| < 0.35, by a polynomial of degree 4 for (1 - e^u) / -u (it
+// interpolates at the Chebyshev points; off by 1.5e-8, in fp32 by 1.3e-7); elsewhere a^2 is at most 0.71 and its roundings count 2.4 times.
 __device__ __forceinline__ float one_minus_square(float q, float a)
 {
-    const float u = 2.f * kLn2 * q;
-    float s = fmaf(u, 1.f / 5040, 1.f / 720);
-    s = fmaf(s, u, 1.f / 120);
-    s = fmaf(s, u, 1.f / 24);
-    s = fmaf(s, u, 1.f / 6);
-    s = fmaf(s, u, 0.5f);
-    s = fmaf(s, u, 1.f);
-    return u > -0.35f ? -u * s : fmaf(-a, a, 1.f);
+    float s = fmaf(q, 0.03692220151424408f, 0.1526535451412201f);
+    s = fmaf(s, q, 0.44392266869544983f);
+    s = fmaf(s, q, 0.9609025716781616f);
+    s = fmaf(s, q, 1.3862943649291992f);
+    return q > -0.25246699f ? -q * s : fmaf(-a, a, 1.f);
 }
 
 template <int CTRL, int ROWS>
