@@ -16,18 +16,22 @@ namespace {
 // same product.  Runs and waves combine both in one exchange: forwards inside 64 tokens, from the state that the forward pass left ahead of them, backwards through the whole
 // tile.  What the gradients take of the gates is formed on the first walk, so that nothing of a token is worked out twice.
 // OUT false: only the pairs (P, R) of whole segments, of all but the first.
-template <int IO, int W, bool LRU, bool HASI, bool HASZ, bool OUT>
-__global__ __launch_bounds__(64 * W) void gated_backward_kernel(const GatedGradParams p)
+template <int IO, int CL, int W, bool LRU, bool HASI, bool HASZ, bool OUT>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(CL == 32 ? 4 : 2))) void gated_backward_kernel(const GatedGradParams p)
 {
-    using Ln = GatedLane<IO>;
-    constexpr int CH = Ln::CH, T = W * kWaveTokens, K = kRun;
-    static_assert(W % kBlockWaves == 0, "tiles are whole blocks of 64 tokens");
-    __shared__ __attribute__((aligned(16))) float pairs[2][W][kLanes][3 * CH];
-    __shared__ __attribute__((aligned(16))) uint32_t ahead[OUT ? 3 + HASI + HASZ : 2 + HASZ][K][W][64];       // the next tile's values, on their way: each wave's own
-    const unsigned lane = threadIdx.x & 63u, cl = lane % kLanes, run = lane / kLanes;
+    using Ln = GatedLane<IO, CL>;
+    constexpr int CH = Ln::CH, T = W * Ln::WT, K = kRun;
+    constexpr int BW = SSMV_GATED_TILE / Ln::WT;                    // waves that share a state of the forward pass
+    static_assert(W % BW == 0, "tiles are whole blocks of 64 tokens");
+    __shared__ __attribute__((aligned(16))) float pairs[2][W][CL][3 * CH];
+    // the next tile's values, on their way, and the states ahead of its blocks of 64 tokens: each wave's own
+    constexpr int TENSORS = OUT ? 3 + HASI + HASZ : 2 + HASZ, WORDS = TENSORS * K + (OUT ? CH : 0);
+    __shared__ __attribute__((aligned(16))) uint32_t ahead[WORDS][W][64];
+    const unsigned lane = threadIdx.x & 63u, cl = lane % CL;
+    unsigned run = lane / CL;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int first = (int)xcd_contiguous(blockIdx.x, gridDim.x) * Ln::CW, seg = OUT ? blockIdx.y : blockIdx.y + 1;
-    const Ln ln(first + (int)cl * CH, p.C);
+    Ln ln(first + (int)cl * CH, p.C);
     int b = blockIdx.z;
     if (p.seq_len && p.batch > 1 && p.batch <= 64) b = __builtin_amdgcn_readfirstlane(zth_longest(p.seq_len, p.batch, b, lane));
     const int all = p.seq_len ? min(max(p.seq_len[b], 0), p.L) : p.L;
@@ -49,6 +53,11 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(const GatedGradP
     }
     if (p.f_bias) ln.floats(p.f_bias, fb);
     if (HASI && p.i_bias) ln.floats(p.i_bias, ib);
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {                                  // as exponents of 2
+        fb[c] *= -kLog2e;
+        ib[c] *= -kLog2e;
+    }
     if (have && (OUT || len == all)) {
         if (p.dh_out) ln.floats(p.dh_out + (size_t)b * p.C, carry);
         if (OUT)
@@ -63,14 +72,14 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(const GatedGradP
     }
 
     const size_t blocks = (p.L + SSMV_GATED_TILE - 1) / SSMV_GATED_TILE;
-    const int wave0 = wave * kWaveTokens, run0 = wave0 + (int)run * K;
+    const int wave0 = wave * Ln::WT, run0 = wave0 + (int)run * K;
     // the last tile, where it is not whole (all of them of a row of one bf16 channel), then whole ones
     const int n = have ? len - from : 0, whole = p.C >= CH ? n - n % T : 0;
     int t0 = from + (n + T - 1) / T * T - T;
     const size_t tok0 = (size_t)b * p.L + wave0 + t0;               // of a tile that is there, but where there is none
-    Walk<IO> wx(p.x, p.x_stride, tok0, run, ln), wf(p.f, p.f_stride, tok0, run, ln), wi(p.i, p.i_stride, tok0, run, ln), wz(p.z, p.z_stride, tok0, run, ln),
+    Walk<IO, CL> wx(p.x, p.x_stride, tok0, run, ln), wf(p.f, p.f_stride, tok0, run, ln), wi(p.i, p.i_stride, tok0, run, ln), wz(p.z, p.z_stride, tok0, run, ln),
         wy(p.dy, p.dy_stride, tok0, run, ln);
-    Walk<IO> wdx(p.dx, p.dx_stride, tok0, run, ln), wdf(p.df, p.df_stride, tok0, run, ln), wdi(p.di, p.di_stride, tok0, run, ln), wdz(p.dz, p.dz_stride, tok0, run, ln);
+    Walk<IO, CL> wdx(p.dx, p.dx_stride, tok0, run, ln), wdf(p.df, p.df_stride, tok0, run, ln), wdi(p.di, p.di_stride, tok0, run, ln), wdz(p.dz, p.dz_stride, tok0, run, ln);
     uint32_t rx[K], rf[K], ri[K], rz[K], ry[K];
     float block[CH];                                                // the state ahead of the lane's block of 64 tokens
     auto each = [&](auto &&fn) {                                    // the tensors of a tile
@@ -80,23 +89,29 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(const GatedGradP
         if (OUT) fn(wx, rx, 2 + HASZ);
         if (OUT && HASI) fn(wi, ri, 3 + HASZ);
     };
-    // of a block that has no token the last block's, which nothing comes of
-    auto state = [&](int t0) { if (OUT) ln.floats(p.states + ((size_t)b * blocks + min(t0 + wave0, len - 1) / SSMV_GATED_TILE) * p.C, block); };
+    auto block_of = [&](int t0) { return p.states + ((size_t)b * blocks + (t0 + wave0) / SSMV_GATED_TILE) * p.C; };
     auto fetch_tail = [&](int t0) {
-        state(t0);
+        if (OUT) ln.floats(block_of(min(t0, len - 1 - wave0)), block);       // of a block that has no token the last block's, which nothing comes of
         each([&](auto &w, uint32_t (&r)[K], int) {
             w.load_tail(r, t0 + wave0, run, len, ln);
             w.move(-T);
+#pragma unroll
+            for (int k = 0; k < K; ++k) asm volatile("" : "+v"(r[k]));
         });
     };
+    const unsigned state_off = (unsigned)ln.c0 * 4;
     auto prefetch = [&](int t0) {
-        state(t0);
         each([&](auto &w, uint32_t (&)[K], int i) {
-            w.prefetch(&ahead[i][0][wave][0], W * 64);
+            w.prefetch(&ahead[i * K][wave][0], W * 64);
             w.move(-T);
         });
+        if (OUT) {
+            const char *row = reinterpret_cast<const char *>(block_of(t0));
+#pragma unroll
+            for (int c = 0; c < CH; ++c) load_to_lds(row + 4 * c, state_off, &ahead[TENSORS * K + c][wave][0]);
+        }
     };
-    auto tile = [&](auto tail, int t0, int buf, auto &&next) {
+    auto tile = [&](auto tail, int t0, int buf) {
         constexpr bool TAIL = decltype(tail)::value;
         const int t = t0 + run0;
         float a[K][CH], g[K][CH], v[OUT ? K : 1][CH], zz[OUT ? K : 1][CH];
@@ -113,7 +128,9 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(const GatedGradP
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 float r, nr, q = 0.f, m = 0.f, m2 = 0.f;
-                sigmoids(f[c] + fb[c], r, nr);
+                const float fe = fmaf(f[c], -kLog2e, fb[c]);
+                if (LRU) sigmoid_pair(__builtin_amdgcn_exp2f(fe), r, nr);
+                else sigmoids_log2(fe, r, nr);
                 a[k][c] = r;
                 if (LRU) {
                     q = rate[c] * r;
@@ -127,7 +144,7 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(const GatedGradP
                 }
                 if (OUT) {
                     float si = 1.f, ni = 0.f;
-                    if (HASI) sigmoids(i[c] + ib[c], si, ni);
+                    if (HASI) sigmoid_pair(__builtin_amdgcn_exp2f(fmaf(i[c], -kLog2e, ib[c])), si, ni);
                     const float u = HASI ? x[c] * si : x[c];
                     if (LRU) {
                         m2 = one_minus_square(q, a[k][c]);
@@ -151,6 +168,23 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(const GatedGradP
             }
         }
 #pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                constexpr int O = OUT ? 1 : 0;
+                settle(a[k][c]);
+                settle(g[k][c]);
+                if (OUT) {
+                    settle(v[O * k][c]);
+                    settle(e0[O * k][c]);
+                    settle(e1[O * k][c]);
+                    if (LRU) settle(e2[O * k][c]);
+                    settle(ex[O * k][c]);
+                    if (HASI) settle(ei[O * k][c]);
+                    if (HASZ) settle(zz[O * k][c]);
+                }
+            }
+#pragma unroll
         for (int c = 0; c < CH; ++c) begin[c] = block[c];
         if (TAIL) {                                                 // tokens that are none: nothing flows into them, and through them as it is
 #pragma unroll
@@ -167,7 +201,6 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(const GatedGradP
                     }
                 }
         }
-        next();
         float Pf[CH], Hf[CH], Pr[CH], Rr[CH], Pt[CH], Ht[CH], Rt[CH];
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
@@ -178,8 +211,8 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(const GatedGradP
                 if (OUT) H = fmaf(a[k][c], H, v[OUT ? k : 0][c]);
                 R = a[K - 1 - k][c] * (g[K - 1 - k][c] + R);
             }
-            combine_forward(P, H, run, Pf[c], Hf[c], Pt[c], Ht[c]);
-            combine_backward(P, R, run, Pr[c], Rr[c], Rt[c]);
+            combine_forward<CL>(P, H, run, Pf[c], Hf[c], Pt[c], Ht[c]);
+            combine_backward<CL>(P, R, run, Pr[c], Rr[c], Rt[c]);
         }
         if (run == 0) {
 #pragma unroll
@@ -199,10 +232,12 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(const GatedGradP
                 const float pw = pairs[buf][w][cl][c];
                 carry[c] = fmaf(pw, carry[c], pairs[buf][w][cl][CH + c]);
                 if (!OUT) prod[c] *= pw;
+                settle(carry[c]);
+                settle(flow[c]);
             }
         }
         if constexpr (OUT) {
-            for (int w = wave / kBlockWaves * kBlockWaves; w < wave; ++w)
+            for (int w = wave / BW * BW; w < wave; ++w)
 #pragma unroll
                 for (int c = 0; c < CH; ++c) begin[c] = fmaf(pairs[buf][w][cl][c], begin[c], pairs[buf][w][cl][2 * CH + c]);
 #pragma unroll
@@ -219,7 +254,7 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(const GatedGradP
                     begin[c] = fmaf(a[k][c], begin[c], v[k][c]);
                     if (HASZ) zz[k][c] *= begin[c];
                 }
-            if (HASZ && p.dz) wdz.template store<TAIL>(zz, t0 + wave0, run, len, ln);
+            if (HASZ && p.dz) wdz.template store<TAIL>(zz, t0 + wave0, run, len, ln, false);
 #pragma unroll
             for (int k = K - 1; k >= 0; --k)
 #pragma unroll
@@ -238,9 +273,9 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(const GatedGradP
                     }
                     sumF[c] += e0[k][c];
                 }
-            if (p.dx) wdx.template store<TAIL>(ex, t0 + wave0, run, len, ln);
-            if (p.df) wdf.template store<TAIL>(e0, t0 + wave0, run, len, ln);
-            if (HASI && p.di) wdi.template store<TAIL>(ei, t0 + wave0, run, len, ln);
+            if (p.dx) wdx.template store<TAIL>(ex, t0 + wave0, run, len, ln, false);
+            if (p.df) wdf.template store<TAIL>(e0, t0 + wave0, run, len, ln, false);
+            if (HASI && p.di) wdi.template store<TAIL>(ei, t0 + wave0, run, len, ln, false);
             wdx.move(-T);
             wdf.move(-T);
             wdi.move(-T);
@@ -251,28 +286,31 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(const GatedGradP
     const std::false_type full{};
     int buf = 0;
     for (; t0 >= from + whole; t0 -= T, buf ^= 1) {
+        asm volatile("" : "+v"(ln.c0), "+v"(ln.skip), "+v"(run));   // what only this loop needs of them is worked out in it
         fetch_tail(t0);
-        tile(tail, t0, buf, [] {});
+        tile(tail, t0, buf);
     }
     if (whole > 0) {
+        // Behind a tile's loads a wave has issued the stores of the tile before: how many is known where every lane of the workgroup stores and all gradients are wanted.
+        const bool known = OUT && first + Ln::CW <= p.C && p.dx && p.df && (!HASI || p.di) && (!HASZ || p.dz);
         prefetch(t0);
-        // behind a tile's loads a wave issues the stores of the tile before it; how many is known where every lane of the workgroup stores and all gradients are wanted
-        const bool known = first + Ln::CW <= p.C && p.dx && p.df && (!HASI || p.di) && (!HASZ || p.dz);
         bool stored = false;
         for (; t0 >= from; t0 -= T, buf ^= 1) {
-            if (OUT && known && stored) wait_but<K * (2 + HASI + HASZ)>();
+            if (known && stored) wait_but<K * (2 + HASI + HASZ)>();
             else wait_but<0>();
+            stored = true;
             each([&](auto &, uint32_t (&r)[K], int i) {
 #pragma unroll
-                for (int k = 0; k < K; ++k) r[k] = ahead[i][k][wave][lane];
+                for (int k = 0; k < K; ++k) r[k] = ahead[i * K + k][wave][lane];
             });
-            tile(full, t0, buf, [&] {
-                if (t0 > from) {
-                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // what is there has been read
-                    prefetch(t0 - T);
-                }
-            });
-            stored = true;
+            if (OUT)
+#pragma unroll
+                for (int c = 0; c < CH; ++c) block[c] = __uint_as_float(ahead[OUT ? TENSORS * K + c : 0][wave][lane]);
+            if (t0 > from) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");              // what is there has been read
+                prefetch(t0 - T);
+            }
+            tile(full, t0, buf);
         }
     }
     if constexpr (!OUT) {
@@ -291,8 +329,8 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(const GatedGradP
             sums[2][c] = sumI[c];
 #pragma unroll
             for (int k = 0; k < 3; ++k) {
-                sums[k][c] += __shfl_xor(sums[k][c], 16);
-                sums[k][c] += __shfl_xor(sums[k][c], 32);
+#pragma unroll
+                for (int d = CL; d < 64; d *= 2) sums[k][c] += __shfl_xor(sums[k][c], d);
                 if (run == 0) pairs[0][wave][cl][k * CH + c] = sums[k][c];
             }
         }
@@ -308,32 +346,32 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(const GatedGradP
     }
 }
 
-template <int IO, int W, bool LRU, bool HASI, bool HASZ>
+template <int IO, int CL, int W, bool LRU, bool HASI, bool HASZ>
 int launch(const GatedGradParams &p, hipStream_t stream)
 {
-    constexpr int CW = GatedLane<IO>::CW;
+    constexpr int CW = GatedLane<IO, CL>::CW;
     const unsigned groups = (unsigned)((p.C + CW - 1) / CW);
     const dim3 block(64 * W);
     if (p.seg_count > 1) {
-        hipLaunchKernelGGL((gated_backward_kernel<IO, W, LRU, false, HASZ, false>), dim3(groups, p.seg_count - 1, p.batch), block, 0, stream, p);
+        hipLaunchKernelGGL((gated_backward_kernel<IO, CL, W, LRU, false, HASZ, false>), dim3(groups, p.seg_count - 1, p.batch), block, 0, stream, p);
         const int e = (int)hipGetLastError();
         if (e != 0) return e;
     }
-    hipLaunchKernelGGL((gated_backward_kernel<IO, W, LRU, HASI, HASZ, true>), dim3(groups, p.seg_count, p.batch), block, 0, stream, p);
+    hipLaunchKernelGGL((gated_backward_kernel<IO, CL, W, LRU, HASI, HASZ, true>), dim3(groups, p.seg_count, p.batch), block, 0, stream, p);
     return (int)hipGetLastError();
 }
 
-template <int IO, int W, bool LRU>
+template <int IO, int CL, int W, bool LRU>
 int launch_gates(const GatedGradParams &p, hipStream_t stream)
 {
-    if (p.i) return p.z ? launch<IO, W, LRU, true, true>(p, stream) : launch<IO, W, LRU, true, false>(p, stream);
-    return p.z ? launch<IO, W, LRU, false, true>(p, stream) : launch<IO, W, LRU, false, false>(p, stream);
+    if (p.i) return p.z ? launch<IO, CL, W, LRU, true, true>(p, stream) : launch<IO, CL, W, LRU, true, false>(p, stream);
+    return p.z ? launch<IO, CL, W, LRU, false, true>(p, stream) : launch<IO, CL, W, LRU, false, false>(p, stream);
 }
 
 template <int IO, bool LRU>
-int launch_waves(const GatedGradParams &p, hipStream_t stream)
+int launch_width(const GatedGradParams &p, hipStream_t stream)
 {
-    return p.waves == 4 ? launch_gates<IO, 4, LRU>(p, stream) : launch_gates<IO, 8, LRU>(p, stream);
+    return p.wide ? launch_gates<IO, 32, 8, LRU>(p, stream) : launch_gates<IO, 16, 8, LRU>(p, stream);
 }
 
 }  // namespace
@@ -341,8 +379,8 @@ int launch_waves(const GatedGradParams &p, hipStream_t stream)
 int launch_gated_backward(const GatedGradParams &p, hipStream_t stream)
 {
     int e;
-    if (p.io == SSMV_BF16) e = p.lru ? launch_waves<SSMV_BF16, true>(p, stream) : launch_waves<SSMV_BF16, false>(p, stream);
-    else e = p.lru ? launch_waves<SSMV_F32, true>(p, stream) : launch_waves<SSMV_F32, false>(p, stream);
+    if (p.io == SSMV_BF16) e = p.lru ? launch_width<SSMV_BF16, true>(p, stream) : launch_width<SSMV_BF16, false>(p, stream);
+    else e = p.lru ? launch_width<SSMV_F32, true>(p, stream) : launch_width<SSMV_F32, false>(p, stream);
     if (e != 0 || !p.partial) return e;
     const ColumnSums to{{p.dA, p.df_bias, p.di_bias}, {p.A, nullptr, nullptr}};
     return launch_column_sums(p.partial, p.batch * p.seg_count, p.C, to, stream);

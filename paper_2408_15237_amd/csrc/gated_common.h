@@ -5,17 +5,15 @@
 
 namespace ssmv {
 
-constexpr int kRun = 4, kLanes = 16, kRuns = 64 / kLanes;      // tokens that a lane takes one after the other; lanes over the channels; runs of a wave
-constexpr int kWaveTokens = kRun * kRuns;
-constexpr int kBlockWaves = SSMV_GATED_TILE / kWaveTokens;     // waves that share a state of the forward pass
-static_assert(kBlockWaves * kWaveTokens == SSMV_GATED_TILE, "tile");
+constexpr int kRun = 4;      // tokens that a lane takes one after the other
 
-// A lane owns 4 bytes of a token's row (two bf16 channels, one fp32) for kRun tokens: lane l of a wave the channels l % 16 and the run l / 16.
+// A lane owns 4 bytes of a token's row (two bf16 channels, one fp32) for kRun tokens: lane l of a wave the channels l % CL and the run l / CL.
 // The last channels of a row are a pair moved back, whose first `skip` channels are another lane's; lanes behind the row have skip >= CH, load what others load and store nothing.
-template <int IO>
+template <int IO, int CL>
 struct GatedLane {
     static constexpr int CH = IO == SSMV_BF16 ? 2 : 1, ES = IO == SSMV_BF16 ? 2 : 4;
-    static constexpr int CW = kLanes * CH;                     // channels of a workgroup
+    static constexpr int CW = CL * CH;                         // channels of a workgroup
+    static constexpr int RUNS = 64 / CL, WT = RUNS * kRun;     // runs and tokens of a wave
 
     int c0, skip, C;
     __device__ __forceinline__ GatedLane(int own, int channels) : c0(max(min(own, channels - CH), 0)), skip(own - c0), C(channels) {}
@@ -44,6 +42,11 @@ struct GatedLane {
         return r;
     }
     static __device__ __forceinline__ void store(char *at, uint32_t r) { __builtin_memcpy(at, &r, 4); }
+    static __device__ __forceinline__ void store_past(char *at, uint32_t r)          // past the caches
+    {
+        typedef uint32_t loose __attribute__((aligned(2)));
+        __builtin_nontemporal_store(r, reinterpret_cast<loose *>(at));
+    }
     // any row
     __device__ __forceinline__ uint32_t load_any(const char *row) const
     {
@@ -83,10 +86,13 @@ __device__ __forceinline__ void load_to_lds(const char *base, unsigned offset, c
 template <int COUNT>
 __device__ __forceinline__ void wait_but() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(COUNT) : "memory"); }
 
+// The value is worked out here: the compiler may not keep its operands instead and finish it where it is used, which costs a register for each of them.
+__device__ __forceinline__ void settle(float &v) { asm volatile("" : "+v"(v)); }
+
 // One tensor of tokens, as a wave walks through it tile by tile: `at` is the wave's first token of a tile.
-template <int IO>
+template <int IO, int CL>
 struct Walk {
-    using Ln = GatedLane<IO>;
+    using Ln = GatedLane<IO, CL>;
     const char *at;
     uint32_t step;           // bytes between tokens
     unsigned off;            // of the lane's run and channels from `at`
@@ -97,8 +103,10 @@ struct Walk {
     __device__ __forceinline__ void load(uint32_t (&r)[kRun]) const
     {
         const char *row = at;
+        unsigned o = off;
+        asm volatile("" : "+v"(o));     // stays a 32-bit offset from a scalar base
 #pragma unroll
-        for (int k = 0; k < kRun; ++k, row += step) r[k] = Ln::load(row + off);
+        for (int k = 0; k < kRun; ++k, row += step) r[k] = Ln::load(row + o);
     }
     // into LDS: the k-th token's words `each` apart
     __device__ __forceinline__ void prefetch(const uint32_t *dst, int each) const
@@ -114,7 +122,7 @@ struct Walk {
         for (int k = 0; k < kRun; ++k) r[k] = ln.load_any(at + (ptrdiff_t)(min(t + (int)run * kRun + k, len - 1) - t) * (ptrdiff_t)step);
     }
     template <bool TAIL>
-    __device__ __forceinline__ void store(const float (&v)[kRun][Ln::CH], int t, unsigned run, int len, const Ln &ln) const
+    __device__ __forceinline__ void store(const float (&v)[kRun][Ln::CH], int t, unsigned run, int len, const Ln &ln, bool past) const
     {
         char *row = const_cast<char *>(at);
         if constexpr (!TAIL) {
@@ -122,8 +130,13 @@ struct Walk {
 #pragma unroll
             for (int k = 0; k < kRun; ++k) r[k] = Ln::encode(v[k]);
             if (ln.skip == 0) {
+                if (past) {
 #pragma unroll
-                for (int k = 0; k < kRun; ++k, row += step) Ln::store(row + off, r[k]);
+                    for (int k = 0; k < kRun; ++k, row += step) Ln::store_past(row + off, r[k]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < kRun; ++k, row += step) Ln::store(row + off, r[k]);
+                }
             } else if (ln.skip < Ln::CH) {                          // the second of two channels
 #pragma unroll
                 for (int k = 0; k < kRun; ++k, row += step) *reinterpret_cast<uint16_t *>(row + off + 2) = (uint16_t)(r[k] >> 16);
@@ -150,36 +163,57 @@ __device__ __forceinline__ void halves(float v, float &low, float &high)
     high = __uint_as_float(r[1]);
 }
 
-// (P, H) of the four runs of a wave, first to last: that of the runs before the lane's, and of all, in every lane.
+// (P, H) of the 64 / CL runs of a wave, first to last: that of the runs before the lane's, and of all, in every lane.
+template <int CL>
 __device__ __forceinline__ void combine_forward(float P, float H, unsigned run, float &Pe, float &He, float &Pt, float &Ht)
 {
     float p0, p1, h0, h1;
-    rows_of_pair(P, p0, p1);
-    rows_of_pair(H, h0, h1);
-    float pa, pb, ha, hb;                                      // of the first and of the second pair
-    halves(p0 * p1, pa, pb);
-    halves(fmaf(p1, h0, h1), ha, hb);
-    Pt = pa * pb;
-    Ht = fmaf(pb, ha, hb);
-    const bool odd = run & 1, second = run & 2;
-    const float pr = odd ? p0 : 1.f, hr = odd ? h0 : 0.f;       // the run before in the lane's pair
-    Pe = second ? pa * pr : pr;
-    He = second ? fmaf(pr, ha, hr) : hr;
+    if constexpr (CL == 32) {
+        halves(P, p0, p1);
+        halves(H, h0, h1);
+        Pt = p0 * p1;
+        Ht = fmaf(p1, h0, h1);
+        Pe = run ? p0 : 1.f;
+        He = run ? h0 : 0.f;
+    } else {
+        static_assert(CL == 16, "lanes");
+        rows_of_pair(P, p0, p1);
+        rows_of_pair(H, h0, h1);
+        float pa, pb, ha, hb;                                  // of the first and of the second pair
+        halves(p0 * p1, pa, pb);
+        halves(fmaf(p1, h0, h1), ha, hb);
+        Pt = pa * pb;
+        Ht = fmaf(pb, ha, hb);
+        const bool odd = run & 1, second = run & 2;
+        const float pr = odd ? p0 : 1.f, hr = odd ? h0 : 0.f;   // the run before in the lane's pair
+        Pe = second ? pa * pr : pr;
+        He = second ? fmaf(pr, ha, hr) : hr;
+    }
 }
 // (P, R) from the last run to the first: that of the runs behind the lane's, and R of all (the product of all is the forward one's).
+template <int CL>
 __device__ __forceinline__ void combine_backward(float P, float R, unsigned run, float &Pe, float &Re, float &Rt)
 {
     float p0, p1, r0, r1;
-    rows_of_pair(P, p0, p1);
-    rows_of_pair(R, r0, r1);
-    float pa, pb, ra, rb;
-    halves(p0 * p1, pa, pb);
-    halves(fmaf(p0, r1, r0), ra, rb);
-    Rt = fmaf(pa, rb, ra);
-    const bool odd = run & 1, second = run & 2;
-    const float pr = odd ? 1.f : p1, rr = odd ? 0.f : r1;
-    Pe = second ? pr : pb * pr;
-    Re = second ? rr : fmaf(pr, rb, rr);
+    if constexpr (CL == 32) {
+        halves(P, p0, p1);
+        halves(R, r0, r1);
+        Rt = fmaf(p0, r1, r0);
+        Pe = run ? 1.f : p1;
+        Re = run ? 0.f : r1;
+    } else {
+        static_assert(CL == 16, "lanes");
+        rows_of_pair(P, p0, p1);
+        rows_of_pair(R, r0, r1);
+        float pa, pb, ra, rb;
+        halves(p0 * p1, pa, pb);
+        halves(fmaf(p0, r1, r0), ra, rb);
+        Rt = fmaf(pa, rb, ra);
+        const bool odd = run & 1, second = run & 2;
+        const float pr = odd ? 1.f : p1, rr = odd ? 0.f : r1;
+        Pe = second ? pr : pb * pr;
+        Re = second ? rr : fmaf(pr, rb, rr);
+    }
 }
 
 }  // namespace ssmv

@@ -177,7 +177,11 @@ int ssm_gated_recurrence_workspace(int32_t batch, int32_t channels, int32_t L, s
 {
     TRY(check_gated_sizes(batch, channels, L));
     if (!out_bytes) return fail(SSMV_EINVAL, "out_bytes is NULL");
-    *out_bytes = 2 * gated_segments(batch, channels, gated_plan(batch, channels, L, false));
+    *out_bytes = 0;                                                 // enough for either type
+    for (int io : {SSMV_F32, SSMV_BF16}) {
+        const size_t n = 2 * gated_segments(batch, channels, gated_plan(batch, channels, L, io, false));
+        if (n > *out_bytes) *out_bytes = n;
+    }
     return SSMV_OK;
 }
 
@@ -196,8 +200,8 @@ int ssm_gated_recurrence(const ssmv_gated_args *args, void *hip_stream)
     if (a.y_out == a.x || a.y_out == a.f || a.y_out == a.i || a.y_out == a.z) return fail(SSMV_EINVAL, "y_out may not be an input");
     if (a.states && (a.states == a.h_in || a.states == a.h_out)) return fail(SSMV_EINVAL, "states may be neither h_in nor h_out");
     GatedParams p{};
-    const GatedPlan plan = gated_plan(a.batch, a.channels, a.L, false);
-    p.waves = plan.waves; p.seg_len = plan.seg_len; p.seg_count = plan.seg_count;
+    const GatedPlan plan = gated_plan(a.batch, a.channels, a.L, a.io_dtype, false);
+    p.wide = plan.wide; p.seg_len = plan.seg_len; p.seg_count = plan.seg_count;
     if (const size_t each = gated_segments(a.batch, a.channels, plan)) {
         TRY(check_ptr(a.workspace, "workspace (these sequences are cut: ssm_gated_recurrence_workspace)"));
         p.seg_p = static_cast<float *>(a.workspace);
@@ -223,7 +227,11 @@ int ssm_gated_recurrence_backward_workspace(int32_t batch, int32_t channels, int
     TRY(check_gated_sizes(batch, channels, L));
     if (!out_bytes) return fail(SSMV_EINVAL, "out_bytes is NULL");
     size_t at;
-    *out_bytes = gated_backward_layout(batch, channels, gated_plan(batch, channels, L, true), &at);
+    *out_bytes = 0;
+    for (int io : {SSMV_F32, SSMV_BF16}) {
+        const size_t n = gated_backward_layout(batch, channels, gated_plan(batch, channels, L, io, true), &at);
+        if (n > *out_bytes) *out_bytes = n;
+    }
     return SSMV_OK;
 }
 
@@ -258,13 +266,13 @@ int ssm_gated_recurrence_backward(const ssmv_gated_grad_args *args, void *hip_st
     if ((a.dx && (a.dx == a.df || a.dx == a.di || a.dx == a.dz)) || (a.df && (a.df == a.di || a.df == a.dz)) || (a.di && a.di == a.dz))
         return fail(SSMV_EINVAL, "two gradients are one tensor");
     if (a.dh_in && (a.dh_in == a.dh_out || a.dh_in == a.states)) return fail(SSMV_EINVAL, "dh_in may be neither dh_out nor states");
-    const GatedPlan plan = gated_plan(a.batch, a.channels, a.L, true);
+    const GatedPlan plan = gated_plan(a.batch, a.channels, a.L, a.io_dtype, true);
     size_t sums_at;
     gated_backward_layout(a.batch, a.channels, plan, &sums_at);
     const bool vectors = a.dA || a.df_bias || a.di_bias;
     if (vectors || plan.seg_count > 1) TRY(check_ptr(a.workspace, "workspace"));
     GatedGradParams p{};
-    p.waves = plan.waves; p.seg_len = plan.seg_len; p.seg_count = plan.seg_count;
+    p.wide = plan.wide; p.seg_len = plan.seg_len; p.seg_count = plan.seg_count;
     p.seg_p = static_cast<float *>(a.workspace);
     p.seg_r = p.seg_p + sums_at / 2 / sizeof(float);
     p.partial = vectors ? p.seg_p + sums_at / sizeof(float) : nullptr;

@@ -36,7 +36,8 @@ struct GatedParams {
     float *h_out, *states;
     size_t x_stride, f_stride, i_stride, z_stride, y_stride;
     int batch, rows_in, C, L, io, lru;
-    int waves, seg_len, seg_count;       // see GatedPlan
+    int wide, seg_len, seg_count;        // see GatedPlan
+    int past;                // a large output is stored past the caches
     float *seg_p;            // [batch][seg_count][C] products of the segments' decays
     float *seg_h;            // [batch][seg_count][C] end states of the segments from zero (the first one's from its start); last place: the start state
 };
@@ -49,7 +50,7 @@ struct GatedGradParams {
     float *dA, *df_bias, *di_bias, *dh_in;
     size_t x_stride, f_stride, i_stride, z_stride, dy_stride, dx_stride, df_stride, di_stride, dz_stride;
     int batch, C, L, io, lru;
-    int waves, seg_len, seg_count;
+    int wide, seg_len, seg_count;
     float *seg_p;            // [batch][seg_count][C] products of the segments' decays
     float *seg_r;            // [batch][seg_count][C] what flows out of a segment's front when nothing flows into its end
     float *partial;          // [batch][seg_count][3][C] sums for A, f_bias, i_bias of a segment's tokens; NULL: none is wanted
@@ -86,27 +87,36 @@ int launch_column_sums(const float *partial, int parts, int C, const ColumnSums 
 constexpr int kNormParts = 512;
 inline int norm_parts(int rows) { return rows < kNormParts ? rows : kNormParts; }
 
-// How the recurrence is laid on the chip.  16 lanes of a wave lie side by side over the channels (two bf16 channels a lane, or one fp32), the wave's four rows of lanes and
-// the workgroup's waves over the tokens, 4 a lane: 16 tokens a wave and tile.
+// How the recurrence is laid on the chip.  A lane takes 4 bytes of a token's row (two bf16 channels, one fp32) for four tokens.  Wide workgroups are 8 waves whose lanes lie 32 over the
+// channels, 64 tokens a tile; narrow ones lie 16 over the channels, with 16 waves (forward, 256 tokens a tile) or 8 (backward, 128).
 struct GatedPlan {
-    int waves;               // of a workgroup: 4, or 16 (forward) or 8 (backward, which needs more registers)
+    int wide;
     int seg_len, seg_count;  // tokens of a segment (whole tiles), segments of the longest sequence
 };
-inline GatedPlan gated_plan(int batch, int C, int L, bool backward)
+// Width and segments: the least time by a model whose constants were measured (LRU with both gates, bf16).  A workgroup that shares a compute unit with few others takes `lone` us a tile,
+// a chip with g of them g / 256 times `busy` where that is more.  A cut sequence costs a pass over all segments but one for their pairs (0.65 of a full one) and 5 us.
+// (us, forward, wide whole / narrow whole / best cut: 1 x 2048 x 8192 62 / 50 / 61, 1 x 2048 x 4096 62 / 44 / 38, 1 x 2048 x 1024 59 / 33 / 17, 8 x 2048 x 5120 196 / 233 / 258,
+//  2 x 8192 x 2048 233 / 158 / 118; backward: 1 x 2048 x 8192 139 / 96 / 105, 1 x 2048 x 1024 127 / 84 / 28, 8 x 2048 x 5120 386 / 443 / 434.)
+inline GatedPlan gated_plan(int batch, int C, int L, int io, bool backward)
 {
-    // counted in fp32 lanes, so that the plan, and with it the workspace, does not depend on the type
-    const long groups = (long)batch * ((C + 15) / 16);
-    GatedPlan r{4, L, 1};
-    if (groups < 1024 && L > 64) r.waves = backward ? 8 : 16;
-    const int tile = 16 * r.waves, tiles = (L + tile - 1) / tile;
-    int want = 1;
-    while (want < 32 && groups * want < 256 && tiles >= 4 * want) want *= 2;
-    if (want > 1) {
-        r.seg_len = (tiles + want - 1) / want * tile;
-        r.seg_count = (L + r.seg_len - 1) / r.seg_len;
-        if (r.seg_count == 1) r.seg_len = L;
+    const int ch = io == SSMV_BF16 ? 2 : 1;
+    GatedPlan best{1, L, 1};
+    double least = 1e30;
+    for (int wide = 1; wide >= 0; --wide) {
+        const int lanes = wide ? 32 : 16, tile = wide ? 64 : backward ? 128 : 256, tiles = (L + tile - 1) / tile;
+        const double groups = (double)batch * ((C + lanes * ch - 1) / (lanes * ch));
+        const double lone = backward ? (wide ? 4.2 : 5.3) : (wide ? 1.95 : 5.0), busy = backward ? (wide ? 4.7 : 6.0) : (wide ? 2.3 : 6.2);
+        for (int want = 1; want <= 32 && want <= tiles; want *= 2) {
+            const int per = (tiles + want - 1) / want, count = (tiles + per - 1) / per;
+            auto pass = [&](double g) { return per * (g / 256 * busy > lone ? g / 256 * busy : lone); };
+            const double us = pass(groups * count) + (count > 1 ? 0.65 * pass(groups * (count - 1)) + 5.0 : 0.0);
+            if (us < least) {
+                least = us;
+                best = GatedPlan{wide, count > 1 ? per * tile : L, count};
+            }
+        }
     }
-    return r;
+    return best;
 }
 
 // ---- device code --------------------------------------------------------------------------------------------------------
@@ -148,12 +158,18 @@ __device__ __forceinline__ void store8(void *base, size_t idx, int live, const f
     }
 }
 
-// sigmoid(v) and 1 - sigmoid(v), both to within a few roundings for every v
-__device__ __forceinline__ void sigmoids(float v, float &s, float &other)
+// sigmoid(-v ln 2) and 1 minus it, both to within a few roundings for every v
+__device__ __forceinline__ void sigmoids_log2(float v, float &s, float &other)
 {
-    const float t = __builtin_amdgcn_exp2f(-kLog2e * fabsf(v)), w = __builtin_amdgcn_rcpf(1.f + t), tw = t * w;
-    s = v < 0.f ? tw : w;
-    other = v < 0.f ? w : tw;
+    const float t = __builtin_amdgcn_exp2f(-fabsf(v)), w = __builtin_amdgcn_rcpf(1.f + t), tw = t * w;
+    s = v > 0.f ? tw : w;
+    other = v > 0.f ? w : tw;
+}
+// sigmoid(v) for e = e^-v, and 1 - sigmoid(v) as e / (1 + e).  Where sigmoid(v) leaves the range of fp32 (v < -87) it is 0 and the other one may be 0, too: for products of both, or with the first.
+__device__ __forceinline__ void sigmoid_pair(float e, float &s, float &other)
+{
+    s = __builtin_amdgcn_rcpf(1.f + e);
+    other = fminf(e, 3e38f) * s;
 }
 __device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * v)); }
 
