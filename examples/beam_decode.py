@@ -3,8 +3,9 @@
 Every layer of the model keeps one state a row: h (fp32) and the newest three conv inputs.  A prompt goes through
 ssm_causal_conv and ssm_selective_scan, a new token through ssm_causal_conv and ssm_selective_step; ssmv_beam_select names for every
 new beam the row that it descends from, and the next step's calls read that row's state.  Nothing is copied to reorder the beams.
+With --repetition, ssmv_logit_rules makes the tokens that a beam's prompt and its own text hold less likely ahead of every choice.
 
-    python examples/beam_decode.py [--layers 4] [--width 1024] [--beams 4] [--prompt 256] [--tokens 32] [--dtype bf16]
+    python examples/beam_decode.py [--layers 4] [--width 1024] [--beams 4] [--prompt 256] [--tokens 32] [--dtype bf16] [--repetition 1.2]
 """
 from __future__ import annotations
 
@@ -87,15 +88,34 @@ class Model:
         return self._norm(last.contiguous(), self.w["norm"]) @ self.w["head"].T
 
 
-def beam_search(model, prompts, lengths, beams, steps, eos):
+class Histories:
+    """What every beam has read and said, and a penalty on its tokens: logits of a token that occurs are divided by it where they are positive, else multiplied."""
+
+    def __init__(self, prompts, lengths, steps, penalty):
+        self.penalty = penalty
+        self.room = prompts.shape[1] + steps
+        self.tokens, self.length = torch.nn.functional.pad(prompts, (0, steps)).contiguous(), lengths.int()
+
+    def apply(self, model, logits, parent, token):
+        rows, i32 = logits.shape[0], dict(dtype=torch.int32, device="cuda")
+        tokens, length = torch.empty(rows, self.room, **i32), torch.empty(rows, **i32)
+        ssmv.ssmv_logit_rules(logits=logits, out=logits, rows=rows, vocab=model.w["vocab"], io=model.io, hist=self.tokens, hist_len=self.length, src_row=parent, token=token,
+                              repetition=torch.full((rows,), self.penalty, device="cuda"), hist_out=tokens, hist_len_out=length)
+        self.tokens, self.length = tokens, length
+
+
+def beam_search(model, prompts, lengths, beams, steps, eos, repetition=None):
     """The `beams` best continuations of every prompt: (tokens [sequences][beams][steps], scores [sequences][beams]), best first.
-    prompts [sequences][n] int32 and lengths [sequences] int32 on the GPU."""
+    prompts [sequences][n] int32 and lengths [sequences] int32 on the GPU.  repetition: a penalty on tokens that occur already, or None."""
     b, vocab = prompts.shape[0], model.w["vocab"]
     i32 = dict(dtype=torch.int32, device="cuda")
     model.reset()
     logits = model.forward(prompts, seq_len=lengths)
     scores, done, rows_in, history = torch.zeros(b, device="cuda"), None, 1, []
+    said = None if repetition is None else Histories(prompts, lengths, steps, repetition)
     for _ in range(steps):
+        if said is not None:
+            said.apply(model, logits, *(history[-1] if history else (None, None)))
         n = b * beams
         parent, token, best, ended = torch.empty(n, **i32), torch.empty(n, **i32), torch.empty(n, device="cuda"), torch.empty(n, **i32)
         work = torch.empty(ssmv.ssmv_beam_workspace(b, rows_in, beams, vocab), dtype=torch.uint8, device="cuda")
@@ -118,15 +138,16 @@ def main():
     for name, value in (("layers", 4), ("width", 1024), ("vocab", 32000), ("sequences", 2), ("beams", 4), ("prompt", 256), ("tokens", 32), ("seed", 0)):
         ap.add_argument("--" + name, type=int, default=value)
     ap.add_argument("--dtype", choices=sorted(IO), default="bf16")
+    ap.add_argument("--repetition", type=float, default=None)
     a = ap.parse_args()
     model = Model(make_weights(a.layers, a.width, 2 * a.width, 16, max(8, a.width // 16 // 8 * 8), a.vocab, a.dtype, a.seed))
     g = torch.Generator().manual_seed(a.seed + 1)
     prompts = torch.randint(3, a.vocab, (a.sequences, a.prompt), generator=g, dtype=torch.int32).cuda()
     lengths = torch.randint(max(1, a.prompt // 2), a.prompt + 1, (a.sequences,), generator=g, dtype=torch.int32).cuda()
-    beam_search(model, prompts, lengths, a.beams, 2, eos=2)
+    beam_search(model, prompts, lengths, a.beams, 2, eos=2, repetition=a.repetition)
     torch.cuda.synchronize()
     began = time.perf_counter()
-    tokens, scores = beam_search(model, prompts, lengths, a.beams, a.tokens, eos=2)
+    tokens, scores = beam_search(model, prompts, lengths, a.beams, a.tokens, eos=2, repetition=a.repetition)
     torch.cuda.synchronize()
     took = time.perf_counter() - began
     for s in range(a.sequences):

@@ -101,6 +101,7 @@ inline GatedPlan gated_plan(int batch, int C, int L, int io, bool backward)
 {
     const int ch = io == SSMV_BF16 ? 2 : 1;
     GatedPlan best{1, L, 1};
+    if (L <= 64) return best;                                       // one tile
     double least = 1e30;
     for (int wide = 1; wide >= 0; --wide) {
         const int lanes = wide ? 32 : 16, tile = wide ? 64 : backward ? 128 : 256, tiles = (L + tile - 1) / tile;

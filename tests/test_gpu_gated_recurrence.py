@@ -138,9 +138,9 @@ def test_parts(io, form, flags):
 
 
 @pytest.mark.parametrize("form", FORMS)
-@pytest.mark.parametrize("b,n,C", [(2, 70, 40000), (600, 70, 34), (300, 150, 60), (40, 300, 150)])
-def test_wide_workgroups(form, b, n, C):
-    """Where there are many channels or sequences, more lanes of a wave lie over the channels: 64, 32 and 16 of them (fp32 and bf16)."""
+@pytest.mark.parametrize("b,n,C", [(2, 70, 40000), (600, 70, 34), (300, 150, 60), (40, 300, 150), (1, 700, 5200), (3, 333, 1001), (1, 1100, 1030), (5, 900, 33)])
+def test_widths(form, b, n, C):
+    """Workgroups of both widths, sequences whole and cut, tails of tokens and channels in each."""
     for io in ("bf16", "f32"):
         _check_forward(b, n, C, io, form, seed=1)
         _check_backward(b, n, C, io, form, seed=1)
