@@ -31,7 +31,7 @@ extern "C" {
  *   n = r * rsqrt(mean(r^2) + eps) * pre_wgt                (pre_wgt NULL: 1)                     -> n_out, the next block's input
  * n is that of r before it is rounded.  x NULL: r = res, the norm ahead of the first block; z, post_wgt, ch_scale and r_out must be NULL.
  * res_dtype: io_dtype or SSMV_F32.  r_out may be res (with one stride).  Squares are summed in fp32: values from about 1e18 on overflow them.
- * eps = 0 leaves a row of zeros without a norm (NaN). */
+ * eps = 0 leaves a row of zeros without a norm (NaN).  rows * ceil(channels / 512) up to 6e7. */
 #define SSMV_BLOCK_NORM_MAX 16384       /* largest `channels` */
 typedef struct ssmv_block_norm_args {
     const void *x;           /* [rows][channels] io_dtype or NULL                                 */

@@ -32,6 +32,8 @@ int check_norm_sizes(int rows, int channels)
 {
     if (rows < 1 || channels < 1) return fail(SSMV_EINVAL, "rows %d and channels %d must be >= 1", rows, channels);
     if (channels > SSMV_BLOCK_NORM_MAX) return fail(SSMV_EUNSUPPORTED, "channels %d > %d", channels, SSMV_BLOCK_NORM_MAX);
+    // a launch counts its threads with 32 bits: 64 for every 512 channels of a row
+    if ((double)rows * ((channels + 511) / 512) * 64 > 4.0e9) return fail(SSMV_EUNSUPPORTED, "%d rows of %d channels: feed them in pieces", rows, channels);
     return SSMV_OK;
 }
 

@@ -72,7 +72,8 @@ RULES = dict(logits=P, out=P + 64, rows=2, vocab=100, io="bf16", hist=P, hist_le
 
 @pytest.mark.parametrize("bad,code", [(dict([(k, P + 1)]), EALIGN) for k in ("x", "z", "res", "post_wgt", "ch_scale", "pre_wgt", "r_out", "n_out")] + [
     (dict(x=None, res=None), EINVAL), (dict(x=None), EINVAL), (dict(x=None, z=None, post_wgt=None, ch_scale=None), EINVAL), (dict(r_out=None, n_out=None), EINVAL),
-    (dict(rows=0), EINVAL), (dict(channels=0), EINVAL), (dict(channels=16385), EUNSUPPORTED), (dict(io=7), EINVAL), (dict(res_io=7), EINVAL), (dict(io="f32", res_io="bf16"), EINVAL),
+    (dict(rows=0), EINVAL), (dict(channels=0), EINVAL), (dict(channels=16385), EUNSUPPORTED), (dict(rows=1 << 27, channels=8), EUNSUPPORTED),
+    (dict(rows=1 << 23, channels=8192), EUNSUPPORTED), (dict(io=7), EINVAL), (dict(res_io=7), EINVAL), (dict(io="f32", res_io="bf16"), EINVAL),
     (dict(eps=-1.0), EINVAL), (dict(eps=float("nan")), EINVAL), (dict(x_stride=15), EINVAL), (dict(z_stride=-16), EINVAL), (dict(res_stride=1 << 25), EUNSUPPORTED),
     (dict(r_stride=8), EINVAL), (dict(n_stride=8), EINVAL), (dict(r_out=P, res_stride=32), EINVAL), (dict(n_out=P), EINVAL), (dict(r_out=P, res=P + 64), EINVAL),
     (dict(n_out=P + 4096), EINVAL), (dict(res_io="f32", res=P + 2), EALIGN),
@@ -86,6 +87,7 @@ def test_norm_refusals(bad, code):
     (dict(x=None, z=None, post_wgt=None, ch_scale=None, dz=None, dpost_wgt=None, dch_scale=None), EINVAL), (dict(workspace=None), EINVAL), (dict(workspace=P + 8), EALIGN),
     (dict(dx=P), EINVAL), (dict(dz=P + 128), EINVAL), (dict(dres=P + 128), EINVAL), (dict(dx=P + 64), EINVAL), (dict(dx=P + 12288), EINVAL), (dict(dres=P + 64, dres_stride=32), EINVAL),
     (dict(dx=P + 128, dx_stride=32), EINVAL), (dict(dn_stride=4), EINVAL), (dict(rows=-1), EINVAL), (dict(channels=20000), EUNSUPPORTED),
+    (dict(rows=1 << 27), EUNSUPPORTED),
 ])
 def test_norm_gradient_refusals(bad, code):
     assert _code(ssmv.ssmv_block_norm_backward, **{**GRAD, **bad}) == code
