@@ -95,7 +95,9 @@ struct Place {
 };
 
 // Bound by memory: x, z and res in, r and n out.  `waves` waves to a row, as many rows as the workgroup has room for; a thread owns NV times 8 adjacent
-// channels of its row, which stay in registers between the passes.  Everything is requested before the first wait.
+// channels of its row, which stay in registers between the passes.  Everything is requested before the first wait.  16384 x 4096 bf16, sum and norm alone, 537 MB, other tensors in
+// every call: 92 to 95 us, 5.7 TB/s (a copy of 1 GiB 6.1); with gate, norm behind the block and scale 135.  Stores past the caches gave 2 %, and would leave the next product
+// without them.
 template <int IO, int RES, int NV, bool SMALL>
 __global__ __launch_bounds__(1024) void block_norm_kernel(const BlockNormParams p, int waves)
 {
@@ -189,6 +191,8 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(const BlockNormParams 
 //   dpre = sum dn rho r;  with S = sum D sigma a:  dscale = alpha post_wgt S,  dpost = alpha ch_scale S                 (sums over the rows)
 // a and r are formed again from the inputs, which have to be read anyway.  A workgroup walks over rows, the next one's values on their way while it works on this one's;
 // k, pre_wgt and the two sums of a thread's channels stay in registers.  The sums go to `partial` at the end, where a second launch adds them in a fixed order.
+// Bound by memory and the three sums of a row one after the other: 8192 x 5120 bf16 with an fp32 stream, 923 MB, 187 us with the second launch's 5 (a copy's rate: 151).  Steps that it took: loads that
+// wait for no branch 525 -> 261; one sum for dscale and dpost, k and pre_wgt in registers 261 -> 210; one workgroup of more than 8 waves a compute unit, not two in turn, 193.
 template <int IO, int RES, int NV, int MAXW, bool SMALL>
 __global__ __launch_bounds__(64 * MAXW) void block_norm_backward_kernel(const BlockNormGradParams p, int waves)
 {

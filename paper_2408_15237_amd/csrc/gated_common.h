@@ -118,8 +118,16 @@ struct Walk {
     // t: the token at `at`; tokens from `len` on are the last one again
     __device__ __forceinline__ void load_tail(uint32_t (&r)[kRun], int t, unsigned run, int len, const Ln &ln) const
     {
+        const char *row[kRun];
 #pragma unroll
-        for (int k = 0; k < kRun; ++k) r[k] = ln.load_any(at + (ptrdiff_t)(min(t + (int)run * kRun + k, len - 1) - t) * (ptrdiff_t)step);
+        for (int k = 0; k < kRun; ++k) row[k] = at + (ptrdiff_t)(min(t + (int)run * kRun + k, len - 1) - t) * (ptrdiff_t)step;
+        if (Ln::CH == 1 || ln.C >= Ln::CH) {
+#pragma unroll
+            for (int k = 0; k < kRun; ++k) r[k] = Ln::load(row[k] + (size_t)ln.c0 * Ln::ES);
+        } else {
+#pragma unroll
+            for (int k = 0; k < kRun; ++k) r[k] = *reinterpret_cast<const uint16_t *>(row[k]);
+        }
     }
     template <bool TAIL>
     __device__ __forceinline__ void store(const float (&v)[kRun][Ln::CH], int t, unsigned run, int len, const Ln &ln, bool past) const
@@ -142,9 +150,14 @@ struct Walk {
                 for (int k = 0; k < kRun; ++k, row += step) *reinterpret_cast<uint16_t *>(row + off + 2) = (uint16_t)(r[k] >> 16);
             }
         } else {
+            row += (size_t)(run * kRun) * step;
+            const bool both = ln.skip == 0 && ln.C >= Ln::CH;
 #pragma unroll
-            for (int k = 0; k < kRun; ++k)
-                if (t + (int)run * kRun + k < len) ln.store_any(row + (ptrdiff_t)(run * kRun + k) * (ptrdiff_t)step, v[k]);
+            for (int k = 0; k < kRun; ++k, row += step) {
+                if (t + (int)run * kRun + k >= len) continue;
+                if (both) Ln::store(row + (size_t)ln.c0 * Ln::ES, Ln::encode(v[k]));
+                else ln.store_any(row, v[k]);
+            }
         }
     }
 };

@@ -19,9 +19,13 @@ __device__ __forceinline__ void coefficients(float f, float nfb, float rate, flo
     }
 }
 
-// h <- a h + v: a run of tokens is the pair (product of a, state that it leaves from zero), and pairs combine in order.  A lane forms the pair of its run, the runs of a
+// h <- a h + v: a run of tokens is the pair (product of a, state that it leaves from zero), and pairs combine in order.  A lane forms the pair of its run of four, the runs of a
 // wave (permutes) and then the waves of the workgroup combine theirs (LDS, one barrier a tile), and every lane goes through its run again from the state that it starts from.  So a
 // token is read once; the gates stay in registers between the two walks, and the next tile's values are on their way.
+// Many channels: bound by memory.  On a walk down the rows of 5 to 9 tensors, a few channels a workgroup, lines of 128 bytes reach 4.4 TB/s and pieces of 64 bytes 3.5, whatever a lane loads at
+// once; 8 x 2048 x 5120 bf16 with both gates, 839 MB, 191 us, 4.4 TB/s (64-byte pieces 217).  Few: by vector instructions, 40 and 8 transcendental ones a value, of 4 and 16 cycles each:
+// 1 x 2048 x 8192 50 us, where the bytes take 28.
+// Loads into LDS (as the backward pass has them) were slower here, 197 -> 217 and 50 -> 62, and so was a branch in place of the choice of `start` for every w, 62 -> 64.
 // OUT false: only the pairs of whole segments, of all but the last.
 template <int IO, int CL, int W, bool LRU, bool HASI, bool HASZ, bool OUT>
 __global__ __launch_bounds__(64 * W) void gated_recurrence_kernel(const GatedParams p)
@@ -48,18 +52,9 @@ __global__ __launch_bounds__(64 * W) void gated_recurrence_kernel(const GatedPar
         h[c] = rate[c] = fb[c] = ib[c] = 0.f;
         prod[c] = 1.f;
     }
-    if (LRU) {
-        ln.floats(p.A, rate);
-#pragma unroll
-        for (int c = 0; c < CH; ++c) rate[c] = decay_exponent(rate[c]);
-    }
+    if (LRU) ln.floats(p.A, rate);
     if (p.f_bias) ln.floats(p.f_bias, fb);
     if (HASI && p.i_bias) ln.floats(p.i_bias, ib);
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        fb[c] *= -kLog2e;
-        ib[c] *= -kLog2e;
-    }
     if (seg == 0) {
         const int src = p.src_row ? p.src_row[b] : b;
         if (OUT && p.seg_count > 1) ln.floats(p.seg_h + seg0 + (size_t)(p.seg_count - 1) * p.C, h);    // h_out may be h_in, and its writer another workgroup
@@ -167,6 +162,12 @@ __global__ __launch_bounds__(64 * W) void gated_recurrence_kernel(const GatedPar
             wy.move(T);
         }
     };
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {                                  // as exponents of 2
+        if (LRU) rate[c] = decay_exponent(rate[c]);
+        fb[c] *= -kLog2e;
+        ib[c] *= -kLog2e;
+    }
     const std::true_type tail{};
     const std::false_type full{};
     int t0 = from, buf = 0;

@@ -10,7 +10,8 @@ constexpr uint32_t kCount = (1u << 19) - 1, kPrompt = 1u << 19, kOccurs = kCount
 // A workgroup takes N tokens of a row.  It counts the row's history and enters the list of biases in a table in LDS (whole numbers, so that the order of the atomics
 // does not show) and then applies both to its logits: where the mask allows none of 8 they are not read, and in place those that nothing changes are neither read nor written.
 // A row costs little more than its bytes, and the way to them is a chain of dependent loads (the parent's index, its length, its tokens; the mask's row, its bits, the logits):
-// everything is requested as soon as its address is known, the logits before the table is built.
+// everything is requested as soon as its address is known, the logits before the table is built.  128 rows x 128011 bf16 out of place, us: grammars alone 14 (66 MB, 4.8 TB/s), histories of up to
+// 1000 tokens 22, both and 100 biases 24 (45 with the loads where they are used); tables of 8192 tokens 31, of 2048 27.  In place, grammars alone, 64 x 49999: 5.
 template <int IO, int N>
 __global__ __launch_bounds__(256) void logit_rules_kernel(const RulesParams p)
 {
