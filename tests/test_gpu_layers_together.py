@@ -72,7 +72,7 @@ def test_a_training_step():
         ssmv.ssmv_block_norm(x=o, res=r, post_wgt=w["post"], ch_scale=w["scale"], pre_wgt=w["pre"], r_out=r2, n_out=n2, rows=rows, channels=D, io="f32", eps=EPS, res_scale=0.5)
         kept.append((nrm, p, states, y, o, r, st))
         r, nrm = r2, n2
-    assert torch.allclose(nrm.view(b, n, D).cpu().double(), out.detach(), rtol=0, atol=5e-4 * float(out.abs().max()))
+    assert torch.allclose(nrm.view(b, n, D).cpu().double(), out.detach(), rtol=0, atol=5e-4 * float(out.detach().abs().max()))
     got_w, got_h = [None] * layers, [None] * layers
     dr, dn = None, cu(G).view(rows, D).contiguous()
     work = torch.empty(ssmv.ssmv_block_norm_backward_workspace(rows, D), dtype=torch.uint8, device="cuda")
