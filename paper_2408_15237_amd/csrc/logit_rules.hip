@@ -10,8 +10,9 @@ constexpr uint32_t kCount = (1u << 19) - 1, kPrompt = 1u << 19, kOccurs = kCount
 // A workgroup takes N tokens of a row.  It counts the row's history and enters the list of biases in a table in LDS (whole numbers, so that the order of the atomics
 // does not show) and then applies both to its logits: where the mask allows none of 8 they are not read, and in place those that nothing changes are neither read nor written.
 // A row costs little more than its bytes, and the way to them is a chain of dependent loads (the parent's index, its length, its tokens; the mask's row, its bits, the logits):
-// everything is requested as soon as its address is known, the logits before the table is built.  128 rows x 128011 bf16 out of place, us: grammars alone 14 (66 MB, 4.8 TB/s), histories of up to
-// 1000 tokens 22, both and 100 biases 24 (45 with the loads where they are used); tables of 8192 tokens 31, of 2048 27.  In place, grammars alone, 64 x 49999: 5.
+// everything is requested as soon as its address is known, the logits before the table is built.  128 rows x 128011 bf16 out of place, us: grammars alone 13.5 (66 MB, 5 TB/s), histories of up to
+// 1000 tokens 22, both and 100 biases 23 (45 with the loads where they are used); tables of 8192 tokens 31, of 2048 27; workgroups that take several pieces and ask for the next one's
+// logits ahead, of which five run on a compute unit, 26.  In place, grammars alone, 64 x 49999: 5.
 template <int IO, int N>
 __global__ __launch_bounds__(256) void logit_rules_kernel(const RulesParams p)
 {
@@ -31,6 +32,9 @@ __global__ __launch_bounds__(256) void logit_rules_kernel(const RulesParams p)
     int32_t ahead[H];
 #pragma unroll
     for (int k = 0; k < H; ++k) ahead[k] = known && tid + k * 256 < p.room ? hist[tid + k * 256] : -1;       // some of it may lie behind the history
+    const bool listed = bias_token && tid < p.bias_n;
+    const int list0 = listed ? bias_token[tid] : -1;
+    const float bias0 = listed ? p.bias[(size_t)b * p.bias_n + tid] : 0.f;
     const unsigned char *mask = (unsigned)mrow < (unsigned)p.mask_rows && p.mask ? reinterpret_cast<const unsigned char *>(p.mask + (size_t)mrow * p.mask_stride) : nullptr;
     uint32_t bits[V8];
 #pragma unroll
@@ -53,18 +57,15 @@ __global__ __launch_bounds__(256) void logit_rules_kernel(const RulesParams p)
         if (tid == 0) repeats = 0;
         __syncthreads();
         if (bias_token) {
-            for (int j = tid; j < p.bias_n; j += 256) {
-                const unsigned at = (unsigned)bias_token[j] - (unsigned)v0;           // negative tokens: far beyond n
-                if (at < (unsigned)n) {
-                    atomicMax(&table[at], (uint32_t)(4095 - j) << 20);
-                    bias_of[j] = p.bias[(size_t)b * p.bias_n + j];
-                }
-            }
+            auto enter = [&](int token, float bias, int j) {
+                const unsigned at = (unsigned)token - (unsigned)v0;                  // negative tokens: far beyond n
+                if (at >= (unsigned)n) return;
+                if (atomicMax(&table[at], (uint32_t)(4095 - j) << 20) != 0) repeats = 1;
+                bias_of[j] = bias;
+            };
+            enter(list0, bias0, tid);
+            for (int j = tid + 256; j < p.bias_n; j += 256) enter(bias_token[j], p.bias[(size_t)b * p.bias_n + j], j);
             __syncthreads();
-            for (int j = tid; j < p.bias_n; j += 256) {
-                const unsigned at = (unsigned)bias_token[j] - (unsigned)v0;
-                if (at < (unsigned)n && table[at] >> 20 != (uint32_t)(4095 - j)) repeats = 1;
-            }
         }
         if (p.hist) {
             const int len = min(max(said, 0), p.room);
