@@ -198,8 +198,9 @@ __global__ __launch_bounds__(64 * MAXW) void block_norm_backward_kernel(const Bl
 {
     __shared__ float part[2][3][2][kMaxWaves];                      // of even and odd rows: one barrier lies between any two uses of the same
     const unsigned lane = threadIdx.x & 63u;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), sub = wave / waves, first = sub * waves;
-    const int per_wg = (int)(blockDim.x >> 6) / waves;
+    constexpr bool ONE = NV == 2 || MAXW > 8;                       // rows of so many waves have a workgroup to themselves
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), sub = ONE ? 0 : wave / waves, first = sub * waves;
+    const int per_wg = ONE ? 1 : (int)(blockDim.x >> 6) / waves;
     const Place<NV, SMALL> at((wave - first) * 64 + (int)lane, waves * 64, p.C);
     const float inv = 1.f / (float)p.C;
     float sum_pre[NV][8], S[NV][8], kk[NV][8], w1[NV][8];
@@ -227,9 +228,8 @@ __global__ __launch_bounds__(64 * MAXW) void block_norm_backward_kernel(const Bl
     struct Row {
         Eight<IO> x[NV], z[NV], dn[NV];
         Eight<RES> res[NV], dr[NV];
-    } next;
-    auto fetch = [&](Row &f, int row_raw) {
-        const size_t row = min(row_raw, p.rows - 1);                // past the last row: that one again
+    } next{};
+    auto fetch = [&](Row &f, size_t row) {                          // of a row that is there: past the last one nothing is read (where dx is dn or dres dr, that may be stored by now) ...
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             if (p.x) f.x[k].template load<SMALL>(p.x, row * p.x_stride + at.c0[k], p.C);
@@ -240,12 +240,12 @@ __global__ __launch_bounds__(64 * MAXW) void block_norm_backward_kernel(const Bl
         }
     };
     const int step = (int)gridDim.x * per_wg;
-    fetch(next, (int)blockIdx.x * per_wg + sub);
+    if ((int)blockIdx.x * per_wg + sub < p.rows) fetch(next, (int)blockIdx.x * per_wg + sub);
     for (int base = (int)blockIdx.x * per_wg, odd = 0; base < p.rows; base += step, odd ^= 1) {    // the same count for all waves of the workgroup
-        const bool have = base + sub < p.rows;
-        const size_t row = have ? base + sub : p.rows - 1;
+        const bool have = ONE || base + sub < p.rows;               // ... and nothing of it is added: 0 times what is no number would be none
+        const size_t row = base + sub;
         const Row cur = next;
-        if (base + step < p.rows) fetch(next, base + step + sub);
+        if (base + step + sub < p.rows) fetch(next, base + step + sub);
         float a[NV][8], r[NV][8], d[NV][8];
         float sigma = 1.f;
         if (p.x) {
@@ -267,7 +267,6 @@ __global__ __launch_bounds__(64 * MAXW) void block_norm_backward_kernel(const Bl
                 sigma = rsqrtf(ss[0] * inv + p.eps);
             }
         }
-        const float sig = have ? sigma : 0.f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             if (p.res) cur.res[k].get(r[k], at.skip[k]);
@@ -297,7 +296,7 @@ __global__ __launch_bounds__(64 * MAXW) void block_norm_backward_kernel(const Bl
                 }
             }
             row_sums<2>(rs, part[odd][1], first, waves, wave, lane);
-            const float rho = rsqrtf(rs[0] * inv + p.eps), back = rho * rho * (rs[1] * inv), rh = have ? rho : 0.f;
+            const float rho = rsqrtf(rs[0] * inv + p.eps), back = rho * rho * (rs[1] * inv);
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
                 float dn[8];
@@ -305,7 +304,7 @@ __global__ __launch_bounds__(64 * MAXW) void block_norm_backward_kernel(const Bl
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     d[k][j] = fmaf(rho, fmaf(-r[k][j], back, dn[j] * w1[k][j]), d[k][j]);
-                    sum_pre[k][j] = fmaf(dn[j] * rh, r[k][j], sum_pre[k][j]);
+                    if (have) sum_pre[k][j] = fmaf(dn[j] * rho, r[k][j], sum_pre[k][j]);
                 }
             }
         }
@@ -318,7 +317,7 @@ __global__ __launch_bounds__(64 * MAXW) void block_norm_backward_kernel(const Bl
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                S[k][j] = fmaf(d[k][j] * sig, a[k][j], S[k][j]);
+                if (have) S[k][j] = fmaf(d[k][j] * sigma, a[k][j], S[k][j]);
                 d[k][j] *= kk[k][j];
                 gs[0] = fmaf(d[k][j], a[k][j], gs[0]);
             }
