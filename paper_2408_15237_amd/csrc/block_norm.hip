@@ -304,7 +304,7 @@ __global__ __launch_bounds__(64 * MAXW) void block_norm_backward_kernel(const Bl
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     d[k][j] = fmaf(rho, fmaf(-r[k][j], back, dn[j] * w1[k][j]), d[k][j]);
-                    if (have) sum_pre[k][j] = fmaf(dn[j] * rho, r[k][j], sum_pre[k][j]);
+                    if (have) sum_pre[k][j] = fmaf(dn[j], rho * r[k][j], sum_pre[k][j]);      // rho r is near 1, where dn rho may overflow
                 }
             }
         }
@@ -317,7 +317,7 @@ __global__ __launch_bounds__(64 * MAXW) void block_norm_backward_kernel(const Bl
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                if (have) S[k][j] = fmaf(d[k][j] * sigma, a[k][j], S[k][j]);
+                if (have) S[k][j] = fmaf(d[k][j], sigma * a[k][j], S[k][j]);
                 d[k][j] *= kk[k][j];
                 gs[0] = fmaf(d[k][j], a[k][j], gs[0]);
             }

@@ -49,3 +49,20 @@ def test_an_infinite_gradient_of_the_last_row(io, rows, C):
     r = float(t["res"][-1, at]) + 0.5 * float(t["x"][-1, at])
     assert float(got["pre"][at]) == math.copysign(INF, r)
     check(got["pre"][others], type(want["dpre"])(want["dpre"].v[others], want["dpre"].e[others]), "f32", "pre")
+
+
+@pytest.mark.parametrize("rows,C", [(9, 40), (4097, 40), (5, 600), (2049, 600)])
+def test_gradients_that_overflow_in_place(rows, C):
+    """dx over dn and dres over dr, both stored as infinities in the last row: the gradient of pre_wgt, which is finite, has the bits of the call that is not in place."""
+    t, _, up = norm_inputs(rows, C, "bf16", "bf16", rows + C, gate=0, post=0, scale=0)
+    t["x"][-1] *= 1e-3
+    t["res"][-1] *= 1e-3
+    up["dn"][-1] *= 1e37                                            # times rho, about 200: beyond fp32
+    apart, dx, dres = _norm_gradients(t, up, rows, C, "bf16")
+    over, dx2, dres2 = _norm_gradients(t, up, rows, C, "bf16", in_place=True)
+    assert bool(torch.isinf(dx[-1]).any()) and bool(torch.isfinite(dx[:-1]).all())
+    assert bool(torch.isfinite(apart["pre"]).all()) and torch.equal(apart["pre"], over["pre"])
+    for a, b in ((dx, dx2), (dres, dres2)):
+        assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+    want = norm_backward(**t, alpha=0.5, **up)
+    check(apart["pre"], want["dpre"], "f32", "pre")
