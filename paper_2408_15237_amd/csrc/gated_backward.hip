@@ -188,11 +188,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(CL == 32
                     const bool is = t + k < len;
                     a[k][c] = is ? a[k][c] : 1.f;
                     g[k][c] = is ? g[k][c] : 0.f;
-                    if (OUT) {
-                        v[OUT ? k : 0][c] = is ? v[OUT ? k : 0][c] : 0.f;
-                        e0[OUT ? k : 0][c] = is ? e0[OUT ? k : 0][c] : 0.f;
-                        if (HASI) ei[OUT ? k : 0][c] = is ? ei[OUT ? k : 0][c] : 0.f;
-                    }
+                    if (OUT) v[OUT ? k : 0][c] = is ? v[OUT ? k : 0][c] : 0.f;
                 }
         }
         float Pf[CH], Hf[CH], Pr[CH], Rr[CH], Pt[CH], Ht[CH], Rt[CH];
@@ -254,18 +250,19 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(CL == 32
 #pragma unroll
                 for (int c = 0; c < CH; ++c) {
                     const float G = g[k][c] + flow[c];
+                    const bool is = !TAIL || t + k < len;           // 0 times what is no number would be none
                     flow[c] = a[k][c] * G;
                     ex[k][c] *= G;
                     if (HASI) {
                         ei[k][c] *= G;
-                        sumI[c] += ei[k][c];
+                        sumI[c] += is ? ei[k][c] : 0.f;
                     }
                     e0[k][c] *= G * e1[k][c];
                     if (LRU) {
-                        sumA[c] += e0[k][c];
+                        sumA[c] += is ? e0[k][c] : 0.f;
                         e0[k][c] *= e2[k][c];
                     }
-                    sumF[c] += e0[k][c];
+                    sumF[c] += is ? e0[k][c] : 0.f;
                 }
             if (p.dx) wdx.template store<TAIL>(ex, t0 + wave0, run, len, ln, false);
             if (p.df) wdf.template store<TAIL>(e0, t0 + wave0, run, len, ln, false);
