@@ -76,7 +76,7 @@ int ssmv_block_norm_backward_workspace(int32_t rows, int32_t channels, size_t *o
  *   SSMV_GATED_MIX:  decay = sigmoid(f + f_bias),           m = 1 - decay              (A must be NULL)
  *   h <- decay * h + m * sigmoid(i + i_bias) * x            (i NULL: without that sigmoid; i_bias must then be NULL)
  *   y = h * z * sigmoid(z)                                  (y = h where z is NULL)
- * in fp32, y rounded once to io_dtype; m keeps its accuracy where the decay is near 1.  src_row, rows_in, seq_len, h_in and h_out as in
+ * in fp32, y rounded once to io_dtype; m keeps its accuracy where the decay is near 1.  batch up to 65535, channels to 2^22, L to 2^30.  src_row, rows_in, seq_len, h_in and h_out as in
  * ssm_selective_scan: rows continue from rows of h_in, an index outside [0, rows_in) from zeros; sequence b has clamp(seq_len[b], 0, L) tokens, what lies behind them is
  * neither read nor written, h_out is the state after them.  h_out may be h_in where src_row is NULL.  An A of 0 keeps its state and takes nothing in; one of -inf
  * forgets at every token (but where the sigmoid is 0 in fp32: it keeps its state there).
@@ -132,7 +132,7 @@ int ssm_gated_recurrence_backward(const ssmv_gated_grad_args *args, void *hip_st
 int ssm_gated_recurrence_backward_workspace(int32_t batch, int32_t channels, int32_t L, size_t *out_bytes);
 
 /* ---- rules on logits -----------------------------------------------------------------------------------------------------
- * Per row b and token v, in this order, in fp32, rounded once to io_dtype:
+ * Per row b and token v, in this order, in fp32, rounded once to io_dtype (rows up to 65535, vocab to 2^24):
  *   1. v occurs in the row's history:   l <- l > 0 ? l / repetition[b] : l * repetition[b]
  *   2. v occurs c > 0 times behind the history's first prompt_len[b] tokens:   l <- l - frequency[b] * c - presence[b]
  *   3. every place j of the row's list with bias_token[b][j] = v:   l <- l + bias[b][j]  (their sum, in the order of the list)
@@ -144,7 +144,8 @@ int ssm_gated_recurrence_backward_workspace(int32_t batch, int32_t channels, int
  * Tokens outside [0, vocab) in histories and lists count for nothing (a history keeps them).  hist NULL: hist_len, src_row, token, prompt_len, the outputs and the three penalties must be NULL, too.
  * repetition (positive), frequency, presence [rows] or NULL: 1, 0, 0.  prompt_len NULL: 0.
  * mask_row[b] (NULL: b, of at least `rows` mask_rows) is a row of `mask`, a state of the request's grammar; outside [0, mask_rows): no mask.  A mask may leave a row nothing.
- * out may be logits (with one stride): then only what changes is read and written.  Strides: row_stride and out_stride of logits, 0 = vocab; hist_stride 0 is not allowed
+ * out may be logits (with one stride): then only eights of logits (8 j to 8 j + 7 of a row) of which one changes are read and written; the others of these keep their values (a bf16 NaN
+ * may come back with another payload).  Strides: row_stride and out_stride of logits, 0 = vocab; hist_stride 0 is not allowed
  * where hist is given: it is the room of a row of hist and of hist_out; mask_stride in words, 0 = ceil(vocab / 32). */
 #define SSMV_RULES_HISTORY_MAX ((1 << 19) - 2)      /* largest hist_stride */
 #define SSMV_RULES_BIAS_MAX 4095                    /* largest bias_n      */

@@ -191,8 +191,10 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(const BlockNormParams 
 //   dpre = sum dn rho r;  with S = sum D sigma a:  dscale = alpha post_wgt S,  dpost = alpha ch_scale S                 (sums over the rows)
 // a and r are formed again from the inputs, which have to be read anyway.  A workgroup walks over rows, the next one's values on their way while it works on this one's;
 // k, pre_wgt and the two sums of a thread's channels stay in registers.  The sums go to `partial` at the end, where a second launch adds them in a fixed order.
-// Bound by memory and the three sums of a row one after the other: 8192 x 5120 bf16 with an fp32 stream, 923 MB, 187 us with the second launch's 5 (a copy's rate: 151).  Steps that it took: loads that
-// wait for no branch 525 -> 261; one sum for dscale and dpost, k and pre_wgt in registers 261 -> 210; one workgroup of more than 8 waves a compute unit, not two in turn, 193.
+// Bound by memory and the three sums of a row one after the other: 8192 x 5120 bf16 with an fp32 stream, 923 MB, 181 us with the second launch's 5 (a copy's rate: 151), 90 of them vector instructions by the counters.  Steps that it took: loads that
+// wait for no branch 525 -> 261; one sum for dscale and dpost, k and pre_wgt in registers 261 -> 210; one workgroup of more than 8 waves a compute unit, not two in turn, 193; no question which row a wave has where a row takes the workgroup, 181.
+// Above 6144 channels a thread has two vectors of every tensor.  Up to 8192 that fits (4096 x 8192: bf16 120 us, with an fp32 stream 157, fp32 270 with 60 bytes of scratch a lane); above, more than 8 waves leave a
+// thread 128 registers and 396 to 588 bytes of scratch: 4096 x 16384 971, 1201 and 1888 us, 1.1 to 1.2 TB/s.
 template <int IO, int RES, int NV, int MAXW, bool SMALL>
 __global__ __launch_bounds__(64 * MAXW) void block_norm_backward_kernel(const BlockNormGradParams p, int waves)
 {
@@ -448,7 +450,7 @@ template <int IO, int RES>
 int launch_backward(const BlockNormGradParams &q, hipStream_t stream)
 {
     BlockNormGradParams p = q;
-    const RowShape s = row_shape(p.C, 12, 8);                       // more waves leave a thread 128 registers, too few for the loop
+    const RowShape s = row_shape(p.C, 12, 8);                       // one vector a thread in up to 12 waves: more leave a thread 128 registers, too few for the loop
     int wgs = (p.rows + s.per_wg - 1) / s.per_wg;
     const int most = s.nv == 1 && s.waves <= 8 ? kNormParts : kNormParts / 2;     // two workgroups of 8 waves run on a compute unit, one of more
     if (wgs > most) wgs = most;

@@ -17,7 +17,8 @@ namespace {
 // tile.  What the gradients take of the gates is formed on the first walk, so that nothing of a token is worked out twice.
 // Registers decide: nine values of each of a lane's 8 elements live between the two walks.  The next tile's inputs wait in LDS instead, and `settle` keeps the compiler from holding a value's operands
 // until it is used: 241 -> 128 registers, two workgroups a compute unit.  8 x 2048 x 5120 bf16 with both gates, 1.51 GB, 382 us, 4.0 TB/s, of which the same walk without arithmetic takes
-// 345 (see gated_recurrence.hip); it was 1070 with runs of 8 tokens in registers and 431 with 64-byte pieces.  One workgroup alone takes 4.3 us a tile, 60 % of it vector instructions.
+// 345 (see gated_recurrence.hip); it was 1070 with runs of 8 tokens in registers and 431 with 64-byte pieces.  One workgroup alone takes 4.3 us a tile, 60 % of it vector instructions; of the 382 us they
+// are 189 by the counters.
 // OUT false: only the pairs (P, R) of whole segments, of all but the first.
 template <int IO, int CL, int W, bool LRU, bool HASI, bool HASZ, bool OUT>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(CL == 32 ? 4 : 2))) void gated_backward_kernel(const GatedGradParams p)

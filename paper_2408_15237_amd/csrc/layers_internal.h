@@ -93,8 +93,10 @@ struct GatedPlan {
     int wide;
     int seg_len, seg_count;  // tokens of a segment (whole tiles), segments of the longest sequence
 };
-// Width and segments: the least time by a model whose constants were measured (LRU with both gates, bf16).  A workgroup that shares a compute unit with few others takes `lone` us a tile,
-// a chip with g of them g / 256 times `busy` where that is more.  A cut sequence costs a pass over all segments but one for their pairs (0.65 of a full one) and 5 us.
+// Width and segments: the least time by a model whose constants were measured for LRU with both gates in bf16.  The other forms and fp32 take the same plan, which was not looked for among theirs: with fewer
+// tensors or transcendental functions a tile they run ahead of the model's time (1 x 32768 x 1024 MIX without i, us by the model / measured: forward 123 / 95, backward 247 / 163; 4 x 2048 x 5120 fp32 LRU
+// 184 / 192 and 376 / 366).  A workgroup that shares a compute unit with few others takes `lone` us a tile,
+// a chip with g of them g / 256 times `busy` where that is more.  A cut sequence costs a pass over all segments but one for their pairs (0.65 of a full one, whatever it reads) and 5 us.
 // (us, forward, wide whole / narrow whole / best cut: 1 x 2048 x 8192 62 / 50 / 61, 1 x 2048 x 4096 62 / 44 / 38, 1 x 2048 x 1024 59 / 33 / 17, 8 x 2048 x 5120 196 / 233 / 258,
 //  2 x 8192 x 2048 233 / 158 / 118; backward: 1 x 2048 x 8192 139 / 96 / 105, 1 x 2048 x 1024 127 / 84 / 28, 8 x 2048 x 5120 386 / 443 / 434.)
 inline GatedPlan gated_plan(int batch, int C, int L, int io, bool backward)
@@ -182,7 +184,7 @@ __device__ __forceinline__ float decay_exponent(float A)
 }
 
 // 1 - a^2 for a = 2^q, q <= 0.  Near a = 1, where the difference loses it, -expm1(u) at u = 2 q ln 2, |u| < 0.35, by a polynomial of degree 4 for (1 - e^u) / -u (it
-// interpolates at the Chebyshev points; off by 1.5e-8, in fp32 by 1.3e-7); elsewhere a^2 is at most 0.71 and its roundings count 2.4 times.
+// interpolates at the Chebyshev points; with the coefficients as they are stored off by 3.2e-8 of the value, in fp32 by 1.4e-7); elsewhere a^2 is at most 0.71 and its roundings count 2.4 times.
 __device__ __forceinline__ float one_minus_square(float q, float a)
 {
     float s = fmaf(q, 0.03692220151424408f, 0.1526535451412201f);

@@ -11,7 +11,7 @@ constexpr uint32_t kCount = (1u << 19) - 1, kPrompt = 1u << 19, kOccurs = kCount
 // does not show) and then applies both to its logits: where the mask allows none of 8 they are not read, and in place those that nothing changes are neither read nor written.
 // A row costs little more than its bytes, and the way to them is a chain of dependent loads (the parent's index, its length, its tokens; the mask's row, its bits, the logits):
 // everything is requested as soon as its address is known, the logits before the table is built.  128 rows x 128011 bf16 out of place, us: grammars alone 13.5 (66 MB, 5 TB/s), histories of up to
-// 1000 tokens 22, both and 100 biases 19 (45 with the loads where they are used, at 23 by then); tables of 8192 tokens 31, of 2048 27; workgroups that take several pieces and ask for the next one's
+// 1000 tokens 22, both and 100 biases 16 to 19 (45 with the loads where they are used, when the rest took 23); tables of 8192 tokens 31, of 2048 27; workgroups that take several pieces and ask for the next one's
 // logits ahead, of which five run on a compute unit, 26.  In place, grammars alone, 64 x 49999: 5.
 template <int IO, int N>
 __global__ __launch_bounds__(256) void logit_rules_kernel(const RulesParams p)
