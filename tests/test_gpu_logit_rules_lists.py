@@ -41,9 +41,10 @@ def test_sums_in_the_order_of_the_list(V, pick, n, history):
 
 
 @pytest.mark.parametrize("again", ["one", "filled"])
-@pytest.mark.parametrize("n", [100, 4095])
-def test_a_token_listed_again_costs_little(n, again):
-    """One token twice, or half of the list filled up with one: some twenty times the call without at the most (about 100 instructions one after the other for a place that is listed again)."""
+@pytest.mark.parametrize("n,times", [(100, 10), (4095, 60)])
+def test_a_token_listed_again_costs_little(n, times, again):
+    """One token twice, or half of the list filled up with one.  A place that is listed again takes its wave some 130 cycles, one after the other: 50 of them 3 us and 2048 of them 110 us, behind calls of 5 and
+    7 us, which is twice and 16 times as long; so often again is left for a busy machine.  Where every listed token looks for itself in the rest of the list it is 13 and 480 times."""
     rows, V = 64, 8192
     logits = torch.randn(rows, V, device="cuda")
     out, bias, once = torch.empty_like(logits), torch.randn(rows, n, device="cuda"), torch.arange(n, dtype=torch.int32).repeat(rows, 1)
@@ -62,4 +63,4 @@ def test_a_token_listed_again_costs_little(n, again):
             best = min(best, a.elapsed_time(b))
         return best
 
-    assert took(twice) < 20 * took(once)
+    assert took(twice) < times * took(once)
